@@ -322,6 +322,119 @@ ss_status ss_tier_complete(ss_tier *t, int32_t b);
 ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_t bytes,
                             hipStream_t copy_stream, hipEvent_t wait_before, hipEvent_t signal_after);
 
+/* ---- Paged cache ------------------------------------------------------------
+ * K and V that stay on the GPU between rounds (the Active Tail and the
+ * Speculative Frontier of Eq. 8, a draft model's own context) in pages of a few
+ * tokens that a table hands out per request, as bf16 or quantised as they are
+ * written.  ss_cache_write appends rows, ss_cache_read takes rows out as a bf16
+ * chunk (for ss_attend_history_chunk or a migration), ss_cache_attend attends
+ * the pages where they lie: one token per request (plain decoding, drafting) or
+ * a round's candidates.  A page is one contiguous range of bytes, so
+ * ss_download_range and ss_upload_chunk move whole pages between the tiers, in
+ * 8 bits with half the link's bytes and in 4 bits with a quarter.
+ *
+ * Page layout.  Per KV head a block of page_tokens K rows, page_tokens V rows
+ * and, in the scaled formats, page_tokens x 4 K scales and as many V scales; the
+ * heads' blocks follow each other.  A row is the 128 channels of one token:
+ *   SS_CACHE_BF16   256 bytes
+ *   SS_CACHE_MXFP8  128 bytes, OCP e4m3, and 4 scale bytes (one per 32 channels)
+ *   SS_CACHE_MXFP4   64 bytes, OCP e2m1 (channel 2j in the low half of byte j),
+ *                    and 4 scale bytes
+ * A scale byte s stands for 2^(s - 127).  A block of 32 channels is written with
+ * the smallest exponent e >= -111 for which no value exceeds F 2^e (F = 448 in
+ * e4m3, 6 in e2m1) and each value x as x 2^-e rounded to nearest even.  A block
+ * that holds a NaN or an infinity is written as scale byte 255 with codes 0, and
+ * reads as 32 NaNs.  The bf16 format keeps every bit.
+ *
+ * Conventions shared by the calls
+ *   - Rows: request b has the rows row_start[b] .. row_start[b + 1] - 1 of k, v, q
+ *     and out; its row i of n_b stands for the token at position end[b] - n_b + i.
+ *     So with end counting what the cache holds once the rows are in, one pair
+ *     of row_start and end serves the write and the attention of a step.  With
+ *     row_start null every request has max_rows rows.  Rows behind the last
+ *     request's are left as they were, and so is a request's whole output if it
+ *     has no rows.
+ *   - Positions: token t of request b lies in page page_table[b][t / page_tokens]
+ *     at slot t % page_tokens.  A page may serve several requests that only read
+ *     it (a shared prefix); two rows written to one place race.
+ *   - page_table, row_start and end are device arrays, read when the call's
+ *     kernels run: a captured call follows them from replay to replay.  What
+ *     they hold is checked there, not reported: a token whose page number is not
+ *     in [0, num_pages), or whose position is negative or behind the table, is
+ *     not written, reads as zeros and is not seen by the attention.  row_start
+ *     ascends; rows outside [0, num_rows) are never touched.
+ *   - The calls keep no state and wait for nothing; any number may run at once
+ *     on different streams (attentions with a workspace each), ordered by the
+ *     caller where they write or read the same pages.  The stream belongs to the
+ *     current device.  Every call may be captured into a graph.
+ *   - The result does not depend on how the work is split or scheduled: equal
+ *     inputs give equal bits. */
+#define SS_CACHE_BF16 0
+#define SS_CACHE_MXFP8 1
+#define SS_CACHE_MXFP4 2
+
+/* Most requests of one call. */
+#define SS_CACHE_MAX_REQUESTS 4096
+
+typedef struct {
+  int32_t num_requests;     /* B, 1..SS_CACHE_MAX_REQUESTS                     */
+  int32_t num_q_heads;      /* Hq, a multiple of Hkv (attention only)          */
+  int32_t num_kv_heads;     /* Hkv >= 1                                        */
+  int32_t head_dim;         /* d; only 128 is built (else SS_ERR_UNSUPPORTED)  */
+  int32_t format;           /* SS_CACHE_BF16, SS_CACHE_MXFP8 or SS_CACHE_MXFP4 */
+  int32_t page_tokens;      /* tokens of a page: 16, 32, 64, 128 or 256        */
+  int32_t num_pages;        /* pages at `pages`                                */
+  int32_t table_stride;     /* entries of page_table per request               */
+  int64_t page_stride;      /* bytes between pages, a multiple of 16; 0 = the
+                               page's own bytes (a larger one interleaves
+                               several layers' pages)                          */
+  int32_t max_rows;         /* most rows of a request; each request's rows if
+                               row_start is null.  Attention: at most
+                               SS_MAX_CANDIDATES, and max_rows * Hq / Hkv at
+                               most SS_MAX_ROWS_PER_KV_HEAD; a request with
+                               more rows counts there as one without rows      */
+  float softmax_scale;      /* sigma > 0, finite (attention only)              */
+  int32_t causal;           /* attention: 1 = row i sees the tokens up to its
+                               own position, 0 = all end[b]                    */
+} ss_cache_desc;
+
+/* Bytes of one page, 0 if the descriptor is invalid (see ss_last_error). */
+size_t ss_cache_page_bytes(const ss_cache_desc *desc);
+
+/* Write rows into the cache.  k, v: device bf16, row r's KV head h at element
+ * r * row_stride + h * d (row_stride 0: packed, Hkv * d; else a multiple of 8, so
+ * both may be views of a fused projection).  num_rows: rows of k and v. */
+ss_status ss_cache_write(const ss_cache_desc *desc, void *pages, const int32_t *page_table, const void *k, const void *v,
+                         int64_t row_stride, int32_t num_rows, const int32_t *row_start, const int32_t *end,
+                         hipStream_t stream);
+
+/* Read rows out of the cache into a bf16 chunk of num_rows tokens in the given
+ * history layout (SS_KV_TOKEN_MAJOR, SS_KV_HEAD_MAJOR or SS_KV_HEAD_MAJOR_KV with
+ * v = k + d elements).  k, v: device; they must not overlap the pages. */
+ss_status ss_cache_read(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, void *k, void *v,
+                        int32_t kv_layout, int32_t num_rows, const int32_t *row_start, const int32_t *end,
+                        hipStream_t stream);
+
+/* Bytes of device workspace ss_cache_attend needs with this descriptor, whatever
+ * the lengths; 0 if the descriptor is invalid (see ss_last_error). */
+size_t ss_cache_attend_workspace_bytes(const ss_cache_desc *desc);
+
+/* Attend the cache: O = softmax(sigma q K^T) V per query row and head (Eq. 12)
+ * over the tokens that the row sees.  q: device bf16, row r's head h at element
+ * r * q_row_stride + h * d (0: packed, Hq * d).  out: device fp32 [num_rows, Hq,
+ * d].  lse: null or device fp32 [num_rows, Hq], the natural-log sum of exp of the
+ * scaled scores.  A row that sees nothing gets out 0 and lse -inf.
+ * prev_out, prev_lse: both null, or an earlier part's out and lse over other
+ * keys (a round's, or this call's over an earlier chunk of pages); the result is
+ * then of both parts' keys together (Eq. 14).  A part whose lse is -inf does not
+ * count.  They may be out and lse themselves.  workspace: device, 256-byte
+ * aligned, at least ss_cache_attend_workspace_bytes(desc), the call's own until
+ * its work has completed; its contents do not matter. */
+ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const void *q,
+                          int64_t q_row_stride, int32_t num_rows, const int32_t *row_start, const int32_t *end,
+                          float *out, float *lse, const float *prev_out, const float *prev_lse, void *workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
 /* ---- I/O-aware dynamic verification width (paper Sec. 4.2) ----------------
  * Chooses the next round's width q (candidate rows per request, 1..8) as
  * q* = argmin_q T_round(q) / U(q): estimated round time per committed token.

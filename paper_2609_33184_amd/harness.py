@@ -263,3 +263,76 @@ def run_round_single_slot(b: RoundBuffers, host: HostHistory, slot: torch.Tensor
         torch.cuda.synchronize()
         ss.ss_event_destroy(ready)
         ss.ss_event_destroy(free)
+
+
+class PagedCache:
+    """A paged cache with its table and free pages, for a Cohort's requests.
+
+    ``end[b]`` counts request b's tokens on the device, ``tokens[b]`` on the
+    host, so that ``grow`` can hand out pages without waiting for the GPU."""
+
+    def __init__(self, num_requests: int, num_q_heads: int, num_kv_heads: int, max_tokens: int, fmt: int = ss.SS_CACHE_MXFP8,
+                 page_tokens: int = 64, num_pages: Optional[int] = None, max_rows: int = 1,
+                 softmax_scale: Optional[float] = None, causal: int = 1, device="cuda"):
+        width = -(-max_tokens // page_tokens)
+        pages = num_requests * width if num_pages is None else num_pages
+        self.desc = ss.make_cache_desc(num_requests, num_kv_heads, fmt, page_tokens, pages, width, num_q_heads,
+                                       max_rows=max_rows, softmax_scale=softmax_scale, causal=causal)
+        page_bytes = ss.ss_cache_page_bytes(self.desc)
+        ws_bytes = ss.ss_cache_attend_workspace_bytes(self.desc)
+        if page_bytes == 0 or ws_bytes == 0:
+            raise ss.SpecStreamError(ss.SS_ERR_INVALID_ARGUMENT, "PagedCache", ss.ss_last_error())
+        self.pages = torch.empty(pages, num_kv_heads, page_bytes // num_kv_heads, dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
+        self.table = torch.full((num_requests, width), -1, dtype=torch.int32, device=device)
+        self.end = torch.zeros(num_requests, dtype=torch.int32, device=device)
+        self.tokens = [0] * num_requests
+        self.owned: List[List[int]] = [[] for _ in range(num_requests)]
+        self.free = list(range(pages))[::-1]
+
+    def grow(self, rows: Sequence[int]) -> None:
+        """Room for rows[b] more tokens of each request; ``end`` then counts them."""
+        for b, n in enumerate(rows):
+            self.tokens[b] += n
+            need = -(-self.tokens[b] // self.desc.page_tokens)
+            if need > self.table.shape[1] or need - len(self.owned[b]) > len(self.free):
+                raise MemoryError("the cache is full")
+            new = [self.free.pop() for _ in range(need - len(self.owned[b]))]
+            if new:
+                at = len(self.owned[b])
+                self.table[b, at:at + len(new)] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
+                self.owned[b] += new
+        self.end += torch.tensor(list(rows), dtype=torch.int32, device=self.end.device)
+
+    def release(self, rows: Sequence[int]) -> None:
+        """The last rows[b] tokens of each request are rejected: their pages go back."""
+        for b, n in enumerate(rows):
+            self.tokens[b] -= n
+            keep = -(-self.tokens[b] // self.desc.page_tokens)
+            self.free += self.owned[b][keep:]
+            del self.owned[b][keep:]
+        self.end -= torch.tensor(list(rows), dtype=torch.int32, device=self.end.device)
+
+    def _starts(self, row_start: Optional[torch.Tensor]) -> Optional[int]:
+        return None if row_start is None else row_start.data_ptr()
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, stream: int, row_start: Optional[torch.Tensor] = None) -> None:
+        """Rows [T, Hkv, 128] of k and v (views of one projection may be strided alike) enter the cache."""
+        ss.ss_cache_write(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), k.shape[0],
+                          self.end.data_ptr(), self._starts(row_start), k.stride(0), stream)
+
+    def read(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, stream: int, row_start: Optional[torch.Tensor] = None,
+             kv_layout: int = ss.SS_KV_TOKEN_MAJOR, end: Optional[torch.Tensor] = None) -> None:
+        """The rows that end at ``end`` (the cache's own by default) leave as a bf16 chunk."""
+        end = self.end if end is None else end
+        ss.ss_cache_read(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), num_rows,
+                         end.data_ptr(), self._starts(row_start), kv_layout, stream)
+
+    def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
+               row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
+        """out, lse of rows q [T, Hq, 128], joined with ``prev``'s if given."""
+        ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
+                           self.end.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                           self._starts(row_start), None if prev is None else prev[0].data_ptr(),
+                           None if prev is None else prev[1].data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
+                           q.stride(0), stream)

@@ -31,6 +31,10 @@ SS_KV_TOKEN_MAJOR = 0   # history chunk [sum len][Hkv][d]
 SS_KV_HEAD_MAJOR = 1    # history chunk [Hkv][sum len][d]
 SS_KV_HEAD_MAJOR_KV = 2  # history chunk [Hkv][sum len][2][d]: K and V rows of a token adjacent (v = k + d)
 
+SS_CACHE_BF16 = 0       # a cached K or V row as 256 bytes of bf16
+SS_CACHE_MXFP8 = 1      # 128 bytes of e4m3 and one power-of-two scale per 32 channels
+SS_CACHE_MXFP4 = 2      # 64 bytes of e2m1, scaled alike
+
 EXPORTED = (
     "ss_round_workspace_bytes", "ss_round_init", "ss_upload_chunk", "ss_attend_history_chunk",
     "ss_attend_history_chunks",
@@ -40,6 +44,7 @@ EXPORTED = (
     "ss_status_string", "ss_last_error",
     "ss_tier_endpoint", "ss_tier_create", "ss_tier_destroy", "ss_tier_get", "ss_tier_extend", "ss_tier_commit",
     "ss_tier_plan", "ss_tier_complete", "ss_download_range",
+    "ss_cache_page_bytes", "ss_cache_write", "ss_cache_read", "ss_cache_attend_workspace_bytes", "ss_cache_attend",
     "ss_width_create", "ss_width_destroy", "ss_width_observe", "ss_width_select", "ss_width_estimate",
 )
 
@@ -79,6 +84,31 @@ def make_desc(num_cand: Sequence[int], num_q_heads: int, num_kv_heads: int, head
                       mfma_min_rows, kv_layout, balance_permille, counters_zeroed)
     d._keep = arr
     return d
+
+
+class ss_cache_desc(ctypes.Structure):
+    _fields_ = [
+        ("num_requests", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("table_stride", ctypes.c_int32),
+        ("page_stride", ctypes.c_int64),
+        ("max_rows", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+        ("causal", ctypes.c_int32),
+    ]
+
+
+def make_cache_desc(num_requests: int, num_kv_heads: int, format: int, page_tokens: int, num_pages: int,
+                    table_stride: int, num_q_heads: int = 0, head_dim: int = 128, page_stride: int = 0,
+                    max_rows: int = 1, softmax_scale: Optional[float] = None, causal: int = 1) -> ss_cache_desc:
+    """Build a cache descriptor (num_q_heads, softmax_scale and causal matter to the attention only)."""
+    return ss_cache_desc(num_requests, num_q_heads, num_kv_heads, head_dim, format, page_tokens, num_pages, table_stride,
+                         page_stride, max_rows, (head_dim ** -0.5) if softmax_scale is None else softmax_scale, causal)
 
 
 def lib_path() -> str:
@@ -125,6 +155,11 @@ def load() -> ctypes.CDLL:
         "ss_tier_plan": (I32, [P, I32, PI64, PI64]),
         "ss_tier_complete": (I32, [P, I32]),
         "ss_download_range": (I32, [P, P, SZ, P, P, P]),
+        "ss_cache_page_bytes": (SZ, [ctypes.POINTER(ss_cache_desc)]),
+        "ss_cache_write": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, P, I64, I32, P, P, P]),
+        "ss_cache_read": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, P, I32, I32, P, P, P]),
+        "ss_cache_attend_workspace_bytes": (SZ, [ctypes.POINTER(ss_cache_desc)]),
+        "ss_cache_attend": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, I64, I32, P, P, P, P, P, P, P, SZ, P]),
         "ss_width_create": (I32, [ctypes.POINTER(P), PI32, I32, D, I32, D]),
         "ss_width_destroy": (None, [P]),
         "ss_width_observe": (I32, [P, I32, D, D, D, D, D]),
@@ -309,6 +344,37 @@ def ss_download_range(dst_pinned_host: int, src_device: int, nbytes: int, copy_s
                       wait_before: Optional[int] = None, signal_after: Optional[int] = None) -> None:
     _check(load().ss_download_range(dst_pinned_host, src_device, nbytes, copy_stream, wait_before, signal_after),
            "ss_download_range")
+
+
+# ---------------------------------------------------------------------------
+# paged cache (device addresses; page_table, row_start and end are device int32 arrays)
+# ---------------------------------------------------------------------------
+def ss_cache_page_bytes(desc: ss_cache_desc) -> int:
+    return int(load().ss_cache_page_bytes(ctypes.byref(desc)))
+
+
+def ss_cache_write(desc: ss_cache_desc, pages: int, page_table: int, k: int, v: int, num_rows: int, end: int,
+                   row_start: Optional[int] = None, row_stride: int = 0, stream: int = 0) -> None:
+    _check(load().ss_cache_write(ctypes.byref(desc), pages, page_table, k, v, row_stride, num_rows, row_start, end, stream),
+           "ss_cache_write")
+
+
+def ss_cache_read(desc: ss_cache_desc, pages: int, page_table: int, k: int, v: int, num_rows: int, end: int,
+                  row_start: Optional[int] = None, kv_layout: int = SS_KV_TOKEN_MAJOR, stream: int = 0) -> None:
+    _check(load().ss_cache_read(ctypes.byref(desc), pages, page_table, k, v, kv_layout, num_rows, row_start, end, stream),
+           "ss_cache_read")
+
+
+def ss_cache_attend_workspace_bytes(desc: ss_cache_desc) -> int:
+    return int(load().ss_cache_attend_workspace_bytes(ctypes.byref(desc)))
+
+
+def ss_cache_attend(desc: ss_cache_desc, pages: int, page_table: int, q: int, num_rows: int, end: int, out: int,
+                    lse: Optional[int] = None, row_start: Optional[int] = None, prev_out: Optional[int] = None,
+                    prev_lse: Optional[int] = None, workspace: int = 0, workspace_bytes: int = 0, q_row_stride: int = 0,
+                    stream: int = 0) -> None:
+    _check(load().ss_cache_attend(ctypes.byref(desc), pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse,
+                                  prev_out, prev_lse, workspace, workspace_bytes, stream), "ss_cache_attend")
 
 
 # ---------------------------------------------------------------------------
