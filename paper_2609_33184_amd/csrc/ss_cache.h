@@ -45,16 +45,22 @@ struct CacheAttendArgs : CacheArgs {
   int64_t q_row_stride;
   float *out, *lse;                     // lse may be null
   const float *prev_out, *prev_lse;     // both or neither
-  float *part_a, *part_ml;              // states of the pieces: [2 workgroups][M][128], [2 workgroups][M][2]
+  float *part_a, *part_ml;              // states of the pieces: [2 workers][M][128], [2 workers][M][2]
   int32_t Hq, G;
+  uint32_t g_inv;                       // ceil(65536 / G): r / G = r * g_inv >> 16 for r < 64, G <= 64
   int32_t M;                            // rows per KV head: max_rows * G
-  int32_t wgs;                          // workgroups of the attention launch
+  int32_t workers;                      // shares that the call's tiles are cut into
+  int32_t alone;                        // a worker is a wave, not a workgroup
   int32_t causal;
   float scale_log2;                     // softmax_scale * log2(e)
 };
 
-// Workgroups of the attention over a cache of this kind; M query rows per KV head.
-int cache_attend_wgs(int fmt, int B, int Hkv, int capacity, int M);
+// How the attention over a cache of this kind is split; M query rows per KV head.
+struct CacheSplit {
+  int workers;
+  bool alone;
+};
+CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
 
 // Launch wrappers; return hipGetLastError() of the launch.
 hipError_t launch_cache_write(const CacheRowsArgs &p, int fmt, hipStream_t s);

@@ -18,12 +18,15 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace ss {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
@@ -38,23 +41,28 @@ constexpr int kWaves = 4;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Max / sum across the four 16-lane groups of a wave (lanes l, l^16, l^32, l^48).
+// Max / sum across the GROUPS (4 or 2) equal groups of lanes of a wave.
+template <int GROUPS>
 __device__ __forceinline__ float xgroup_max(float x) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  if constexpr (GROUPS == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
+template <int GROUPS>
 __device__ __forceinline__ float xgroup_sum(float x) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  if constexpr (GROUPS == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ s16x4_t lds_read_tr16(const unsigned char *p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s16x4_t *)(reinterpret_cast<uintptr_t>(p)));
+__device__ __forceinline__ s16x4_t lds_read_tr16(uint32_t at) {   // an LDS address
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)at);
 }
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
@@ -72,13 +80,6 @@ __device__ __forceinline__ u32x4_t widen4(uint32_t w, float scale) {
           __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
           __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
           __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
-}
-
-// Rows of request b for the attention: more than max_rows, or fewer than none, count as none.
-__device__ __forceinline__ int rows_of(const CacheArgs &p, int b) {
-  if (p.row_start == nullptr) return p.max_rows;
-  const int n = p.row_start[b + 1] - p.row_start[b];
-  return n < 0 || n > p.max_rows ? 0 : n;
 }
 
 // ---------------------------------------------------------------------------
@@ -291,83 +292,86 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
 // all of its pair writes the result; the others leave their state (m, l, a) in
 // the workspace, at most two per workgroup, and cache_join_kernel merges them.
 //
-// Per tile: S^T = K Q^T with v_mfma_f32_16x16x32_bf16, K straight from memory
-// in the operand's layout (lane (lr, lq) holds 16 bytes of token lr; the
-// channels of a k-step are permuted alike in Q); softmax with one running
-// maximum and sum per row; O^T += V^T P^T, V through LDS and its transpose
-// read, P straight from the score registers.  In a score tile lane (lr, lq)
-// holds tokens 16 u + 4 lq + r of row lr, in O channels 16 db + 4 lq + r.
+// Per tile: S^T = K Q^T, K straight from memory in the operand's layout (a lane
+// holds 16 bytes at a time of one token; the channels of a k-step are permuted
+// alike in Q); softmax with one running maximum and sum per row; O^T += V^T P^T, V
+// through LDS and its transpose read, P straight from the score registers.  Up
+// to 16 rows per KV head use v_mfma_f32_16x16x32_bf16, more v_mfma_f32_32x32x16_bf16
+// (NR rows): its matrix work keeps the SIMD from issuing other instructions for 5
+// ns of 15.4, that of the two smaller ones it replaces for 8.4 (measured beside
+// independent vector instructions).  Lane l: lr = l % NR, lq = l / NR, kGroups =
+// 64 / NR.  In a score tile lane (lr, lq) holds, as score e, token 4 kGroups (e / 4)
+// + 4 lq + e % 4 of row lr; in O, as piece c, channels 4 kGroups c + 4 lq .. + 3.
 //
-// Precision: P enters as three bf16 parts, 24 bits, so that it is as good as
-// fp32 (two parts leave 1.7e-6 of relative error in the result, three 2e-7);
-// sums and accumulators are fp32.  The running maximum moves only where a score
-// passes it by more than 2^8, which keeps a cross-lane maximum and the
-// rescaling out of most tiles; weights up to 2^8 cost no precision.
+// A wave has the loads of its next tile in flight while it works on one, over
+// the end of a piece too, so that a short piece does not wait for memory.
+// Requests of more than 32 rows per KV head are attended by two waves a tile,
+// 32 rows each (HALVES): accumulators of 64 rows would leave one wave per SIMD,
+// whose matrix and vector instructions then wait for each other.
+//
+// Precision: P enters as three bf16 parts cut from its 24 bits, so that it is
+// exact (two parts would leave 1.7e-6 of relative error in the result, against
+// 2e-7 to 5e-7); sums and accumulators are fp32.  The running maximum moves only
+// where a score passes it by more than 2^8, which keeps a cross-lane maximum
+// and the rescaling out of most tiles; weights up to 2^8 cost no precision.
 // ---------------------------------------------------------------------------
 constexpr int kLdsRow = 256;                        // a staged V row, bf16
 constexpr int kVTile = kCacheTile * kLdsRow;
-constexpr int kKept = 7;                            // rows that only some of a request's candidates see
 constexpr int kAwPitch = 132;                       // floats per row of a wave's partial accumulator
 constexpr float kSlack = 8.f;                       // log2 by which weights may pass 1
 constexpr int kMinShare = 4;                        // tiles: one per wave
 
-// LDS: the queries where they do not stay in registers, then the waves' V tiles
-// and kept rows, whose place the waves' states take at a piece's end.
-template <int RB>
+// LDS: the waves' V tiles, whose place the states of two waves take at a piece's end.
+template <int NR, int STREAMS>
 struct AttendLds {
-  static constexpr bool kQueries = RB > 1;
-  static constexpr int kQ = kQueries ? RB * 16 * kLdsRow : 0;
-  static constexpr int kWave = kVTile + kKept * kLdsRow;
-  static constexpr int kMerge = kWaves * RB * 16 * (kAwPitch + 2) * 4;
-  static constexpr int kBytes = kQ + (kWaves * kWave > kMerge ? kWaves * kWave : kMerge);
+  static constexpr int kMerge = STREAMS == 1 ? 0 : 2 * NR * (kAwPitch + 2) * 4;
+  static constexpr int kBytes = kWaves * kVTile > kMerge ? kWaves * kVTile : kMerge;
 };
 
-__device__ __forceinline__ int clamped_end(const CacheArgs &p, int b) {
-  const int e = p.end[b];
-  return e < 0 ? 0 : e > p.capacity ? p.capacity : e;
-}
-__device__ __forceinline__ int tiles_of(const CacheArgs &p, int b) {
-  return rows_of(p, b) == 0 ? 0 : (clamped_end(p, b) + kCacheTile - 1) / kCacheTile;
+// A request as the attention needs it; in a window, lane i holds request base + i.
+struct Request {
+  int rows;      // n_b: 0 if there are more than max_rows or fewer than none
+  int row0;      // its first row
+  int end;       // as given: positions count from it
+  int len;       // tokens that its table reaches
+  int tiles;
+};
+__device__ __forceinline__ Request request_at(const CacheArgs &p, int b) {
+  Request r;
+  const int c = b < p.B ? b : p.B - 1;     // loads without a branch, so that several calls' overlap
+  r.end = p.end[c];
+  if (p.row_start == nullptr) {
+    r.row0 = c * p.max_rows;
+    r.rows = p.max_rows;
+  } else {
+    const int first = p.row_start[c], behind = p.row_start[c + 1];
+    r.row0 = first;
+    r.rows = behind >= first && (int64_t)behind - first <= p.max_rows ? behind - first : 0;
+  }
+  r.rows = b < p.B ? r.rows : 0;
+  r.len = r.end < 0 ? 0 : r.end > p.capacity ? p.capacity : r.end;
+  r.tiles = r.rows == 0 ? 0 : (r.len + kCacheTile - 1) / kCacheTile;
+  return r;
 }
 
-// Tiles of the requests before mine (my requests: tx per, tx per + 1, ...) and of all; every thread of the workgroup.
-struct Count {
-  int before, mine, all, per;
-};
-__device__ __forceinline__ Count count_tiles(const CacheArgs &p, int tx, int *wave_sums) {
-  Count c;
-  c.per = (p.B + kThreads - 1) / kThreads;
-  c.mine = 0;
-  for (int j = 0; j < c.per; ++j) {
-    const int b = tx * c.per + j;
-    if (b < p.B) c.mine += tiles_of(p, b);
-  }
-  int s = c.mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(s, d);
-    if ((tx & 63) >= d) s += o;
-  }
-  if ((tx & 63) == 63) wave_sums[tx >> 6] = s;
-  __syncthreads();
-  int base = 0;
-  c.all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int v = wave_sums[w];
-    base += w < (tx >> 6) ? v : 0;
-    c.all += v;
-  }
-  c.before = base + s - c.mine;
-  return c;
+// Inclusive prefix sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+  return x;
 }
+__device__ __forceinline__ int lane_of(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
 
 __device__ __forceinline__ int share_of(int total, int wgs) {
-  const int s = (total + wgs - 1) / wgs;
+  const int s = (int)(((uint32_t)total + (uint32_t)wgs - 1) / (uint32_t)wgs);
   return s < kMinShare ? kMinShare : s;
 }
 
-// The result of one row: (m, l) of its state in the log2 domain, a / l and what came before it.  v: four channels.
+// The result of one row: (m, l) of its state in the log2 domain, a / l and what came before it.
 struct RowEnd {
   float inv, lse, own, prev;   // 1 / l; of all; weights of this and of the earlier part
 };
@@ -399,448 +403,559 @@ __device__ __forceinline__ f32x4_t row_value(const CacheAttendArgs &p, const Row
   return v;
 }
 
-template <int FMT>
+template <int FMT, int NR>
 struct Tile {   // a wave's loads of one tile
-  static constexpr int kKLoads = FMT == kCacheBf16 ? 4 : FMT == kCacheMx8 ? 2 : 1;   // per 16 tokens
-  static constexpr int kVLoads = 2 * kKLoads;
-  u32x4_t k[2][kKLoads], v[kVLoads];
-  uint32_t ks[2], vs[kVLoads];
+  static constexpr int kBlocks = kCacheTile / NR;                                    // of NR tokens
+  static constexpr int kKLoads = cache_row_bytes(FMT) / 16 / (64 / NR);              // 16 bytes each, per block
+  static constexpr int kVLoads = cache_row_bytes(FMT) / 32;
+  u32x4_t k[kBlocks][kKLoads], v[kVLoads];
+  uint32_t ks[kBlocks], vs[kVLoads];
 };
 
-template <int FMT, int RB>
-__global__ __launch_bounds__(kThreads, RB == 4 || (RB == 2 && FMT == kCacheBf16) ? 1 : 2) void cache_attend_kernel(CacheAttendArgs p) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[AttendLds<RB>::kBytes];
-  __shared__ int wave_sums[kWaves], found[2];
+// Staged V: 16-byte chunk c of row t lies at c ^ swizzle(t), so that neither the
+// rows' stores (whole rows of 16, 2 x 8 or 4 x 4 chunks) nor the transpose reads
+// (8 rows of two chunks, or 4 rows of four) meet in a bank.
+template <int FMT, int NR>
+__device__ __forceinline__ int swizzle(int t) {
+  if constexpr (NR == 32) return FMT == kCacheBf16 ? 4 * (t & 3) + 2 * ((t >> 2) & 1) : 5 * (t & 3);
+  return 2 * (t & 7) ^ (FMT == kCacheMx8 ? t & 1 : FMT == kCacheMx4 ? (t >> 1) & 1 : 0);
+}
+
+template <int NR>
+struct Mfma;
+template <>
+struct Mfma<16> {
+  using Acc = f32x4_t;
+  static constexpr int kDepth = 32;    // of a product
+  static __device__ __forceinline__ Acc run(bf16x8_t a, bf16x8_t b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mfma<32> {
+  using Acc = f32x16_t;
+  static constexpr int kDepth = 16;
+  static __device__ __forceinline__ Acc run(bf16x8_t a, bf16x8_t b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+// p0, p1 as pairs of bf16 whose sum they are: the 24 bits of a fraction in three cuts of eight.
+__device__ __forceinline__ void cut3(float p0, float p1, uint32_t &a, uint32_t &b, uint32_t &c) {
+  const uint32_t w0 = __float_as_uint(p0), w1 = __float_as_uint(p1);
+  a = __builtin_amdgcn_perm(w1, w0, 0x07060302u);                     // the high halves
+  const float r0 = p0 - __uint_as_float(w0 & 0xffff0000u), r1 = p1 - __uint_as_float(w1 & 0xffff0000u);
+  const uint32_t x0 = __float_as_uint(r0), x1 = __float_as_uint(r1);
+  b = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+  const float s0 = r0 - __uint_as_float(x0 & 0xffff0000u), s1 = r1 - __uint_as_float(x1 & 0xffff0000u);
+  c = __builtin_amdgcn_perm(__float_as_uint(s1), __float_as_uint(s0), 0x07060302u);
+}
+
+constexpr int attend_waves(int fmt, int nr) { return fmt == kCacheBf16 ? (nr == 32 ? 1 : 2) : fmt == kCacheMx8 ? 2 : nr == 32 ? 2 : 3; }   // per SIMD
+
+template <int FMT, int NR, int HALVES, int STREAMS>
+__global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_kernel(CacheAttendArgs p) {
+  using Lds = AttendLds<NR, STREAMS>;
+  static_assert(STREAMS * HALVES == kWaves || (STREAMS == 1 && HALVES == 1), "a workgroup's waves, or each for itself");
+  using Acc = typename Mfma<NR>::Acc;
+  __shared__ __attribute__((aligned(256))) unsigned char smem[Lds::kBytes];
   constexpr int kRow = cache_row_bytes(FMT);
-  constexpr int kRows = RB * 16;
+  constexpr int kGroups = 64 / NR;
+  constexpr int kScores = kCacheTile / kGroups;            // of a tile, per lane
+  constexpr int kRegs = NR / kGroups;                      // of an accumulator: scores of NR tokens, or channels
+  constexpr int kAccs = kCacheDim / NR, kChans = kCacheDim / kGroups / 4;   // accumulators of NR channels; 4-channel pieces
+  constexpr int kSteps = kCacheDim / Mfma<NR>::kDepth, kVSteps = kCacheTile / Mfma<NR>::kDepth;
+  constexpr int kPer = 256 / kRow;                         // k-steps that a lane's 16 bytes of K serve
+  constexpr int kLanes = kRow / 16, kStep = 64 / kLanes;   // V: lanes per row, rows per load
+  constexpr bool kAlone = STREAMS == 1;                    // each wave is a worker
   const int thread = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(thread >> 6);
-  int tx = thread;
+  const int half = HALVES == 2 ? w & 1 : 0, ws = kAlone ? 0 : HALVES == 2 ? w >> 1 : w;   // its rows, its tiles
+  const int worker = kAlone ? blockIdx.x * kWaves + w : blockIdx.x;
 
-  // this workgroup's share and where it starts
-  const Count cnt = count_tiles(p, tx, wave_sums);
-  const int total = cnt.all * p.Hkv;
-  const int share = share_of(total, p.wgs);
-  const int64_t first = (int64_t)blockIdx.x * share;
-  if (first >= total) return;
-  int left = total - (int)first < share ? total - (int)first : share;
-  int h = (int)first / cnt.all;
-  const int at = (int)first - h * cnt.all;
-  if (at >= cnt.before && at < cnt.before + cnt.mine) {
-    int t = at - cnt.before, b = tx * cnt.per;
-    for (int n = tiles_of(p, b); t >= n; n = tiles_of(p, b)) {
-      t -= n;
-      ++b;
+  // This worker's share and where it starts; every wave finds it by itself.  The
+  // requests are counted 64 at a time, lane j keeping the tiles of chunk j.
+  Request win;
+  int base = 0, idx, t0, h, left, all;
+  {
+    const int lane = thread & 63;
+    const int chunks = (p.B + 63) / 64;
+    int before = 0, scan;
+    if (chunks == 1) {
+      win = request_at(p, lane);
+      scan = wave_scan(win.tiles);
+      all = lane_of(scan, 63);
+    } else {
+      int sums = 0;
+      for (int j = 0; j < chunks; j += 4) {
+        int t[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = request_at(p, 64 * (j + i) + lane).tiles;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int sum = lane_of(wave_scan(t[i]), 63);
+          sums = lane == j + i ? sum : sums;
+        }
+      }
+      scan = wave_scan(sums);
+      all = lane_of(scan, 63);
     }
-    found[0] = b;
-    found[1] = t;
+    const int total = all * p.Hkv;
+    const int share = share_of(total, p.workers);
+    const int64_t first = (int64_t)worker * share;
+    if (first >= total) return;
+    left = total - (int)first < share ? total - (int)first : share;
+    h = (int)((uint32_t)first / (uint32_t)all);
+    const int at = (int)first - h * all;
+    if (chunks > 1) {
+      const int owner = __builtin_popcountll(__builtin_amdgcn_ballot_w64(scan <= at));
+      before = owner == 0 ? 0 : lane_of(scan, owner - 1);
+      base = 64 * owner;
+      win = request_at(p, base + lane);
+      scan = before + wave_scan(win.tiles);
+    }
+    idx = __builtin_popcountll(__builtin_amdgcn_ballot_w64(scan <= at));
+    t0 = at - (idx == 0 ? before : lane_of(scan, idx - 1));
   }
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(found[0]);
-  int t0 = __builtin_amdgcn_readfirstlane(found[1]);
 
   const int page_tokens = 1 << p.page_shift;
   const uint32_t v_off = (uint32_t)(page_tokens * kRow), ks_off = 2 * v_off, vs_off = ks_off + 4u * (uint32_t)page_tokens;
-  unsigned char *qs = smem, *vs_lds = smem + AttendLds<RB>::kQ + w * AttendLds<RB>::kWave;
-  while (left > 0) {
-    const int tiles = tiles_of(p, b);
-    if (tiles - t0 <= 0) {            // a request without tokens or rows
-      t0 = 0;
-      if (++b == p.B) {
-        b = 0;
-        ++h;
-      }
-      continue;
+  unsigned char *vs_lds = smem + w * kVTile;
+
+  // Pages of a wave's tiles of a piece: tiles k0 .. k0 + 31 after its first, t0
+  // + ws, of a request with `len` tokens; `count` tiles in all.  Lane j holds
+  // half tile j's page, -1 for what is none.
+  auto pages_of = [&](int b, int t0, int len, int count, int k0) {
+    const int lane = thread & 63;
+    const int k = k0 + (lane >> 1);
+    const int64_t tok = (int64_t)(t0 + ws + STREAMS * k) * kCacheTile + 16 * (lane & 1);
+    int id = -1;
+    if (k < count && tok < len) id = p.table[(int64_t)b * p.table_stride + (tok >> p.page_shift)];
+    return id >= 0 && id < p.num_pages ? id : -1;
+  };
+
+  Tile<FMT, NR> cur;
+  uint32_t gone = 0;     // halves of the loaded tile without a page
+  // Where the tile at token tok of head h lies, its pages in lanes j and j + 1 of ids.
+  struct Where {
+    uint8_t *block[2];
+    uint32_t slot[2];
+    int ok[2];           // tokens of each half
+  };
+  auto find = [&](int tok, int len, int h, int ids, int j) {
+    Where at;
+    gone = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int id = lane_of(ids, j + u);
+      const int tu = tok + 16 * u;
+      const int ok = len - tu;
+      at.ok[u] = ok < 0 || id < 0 ? 0 : ok > 16 ? 16 : ok;
+      gone |= (id < 0 ? 1u : 0u) << u;
+      at.slot[u] = (uint32_t)(tu & (page_tokens - 1));
+      at.block[u] = p.pages + (uint64_t)(id < 0 ? 0 : id) * p.page_stride + (uint64_t)h * p.head_bytes;
     }
-    const int piece = tiles - t0 < left ? tiles - t0 : left;
+    return at;
+  };
+  // Issue the loads of its K.  Rows past the request's tokens are whatever the
+  // page holds (page 0 stands in for none): their scores are masked.  A row's
+  // bytes are spread over several loads, so K's go through the caches; V's are
+  // whole lines and stream past them (64 requests in bf16: 665 us, all through
+  // the caches 742; K streamed costs 64 rows in 8 bits 435 -> 530 us).
+  auto load_k = [&](const Where &at) {
+    const int lane = thread & 63, lr = lane % NR, lq = lane / NR;
+#pragma unroll
+    for (int u = 0; u < Tile<FMT, NR>::kBlocks; ++u) {
+      if constexpr (NR == 16) {
+        const __amdgpu_buffer_rsrc_t krs = __builtin_amdgcn_make_buffer_rsrc(at.block[u], (short)0, at.ok[u] > 0 ? (int)p.head_bytes : 0, kBufferFlags);
+        const uint32_t o = (at.slot[u] + lr) * kRow + 16 * lq;
+#pragma unroll
+        for (int s = 0; s < Tile<FMT, NR>::kKLoads; ++s) cur.k[u][s] = __builtin_amdgcn_raw_buffer_load_b128(krs, o + 16 * kGroups * s, 0, 0);
+        if constexpr (FMT != kCacheBf16) cur.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(krs, ks_off + (at.slot[u] + lr) * 4, 0, 0);
+      } else {
+        // the block's two halves may lie in different pages
+        const uint8_t *block = lr < 16 ? at.block[0] : at.block[1];
+        const uint32_t row = (lr < 16 ? at.slot[0] : at.slot[1]) + (lr & 15);
+        const u32x4_t *src = reinterpret_cast<const u32x4_t *>(block + row * kRow + 16 * lq);
+#pragma unroll
+        for (int s = 0; s < Tile<FMT, NR>::kKLoads; ++s) cur.k[u][s] = src[kGroups * s];
+        if constexpr (FMT != kCacheBf16) cur.ks[u] = *reinterpret_cast<const uint32_t *>(block + ks_off + row * 4);
+      }
+    }
+  };
+  // Issue the loads of its V.  Rows past the request's tokens touch no memory and
+  // read zero: a weight of zero must meet no leftover NaN.
+  auto load_v = [&](const Where &at) {
+    const int lane = thread & 63;
+    __amdgpu_buffer_rsrc_t vrs[2], srs[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      vrs[u] = __builtin_amdgcn_make_buffer_rsrc(at.block[u], (short)0, at.ok[u] > 0 ? (int)(v_off + (at.slot[u] + at.ok[u]) * kRow) : 0, kBufferFlags);
+      srs[u] = __builtin_amdgcn_make_buffer_rsrc(at.block[u], (short)0, at.ok[u] > 0 ? (int)(vs_off + (at.slot[u] + at.ok[u]) * 4) : 0, kBufferFlags);
+    }
+#pragma unroll
+    for (int i = 0; i < Tile<FMT, NR>::kVLoads; ++i) {
+      const int u = i * kStep / 16;
+      const uint32_t row = at.slot[u] + (i * kStep) % 16 + lane / kLanes;
+      cur.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vrs[u], v_off + row * kRow + 16 * (lane % kLanes), 0, kStreamLoad);
+      if constexpr (FMT != kCacheBf16)
+        cur.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(srs[u], vs_off + row * 4 + (lane % kLanes) * 4 / kLanes, 0, kStreamLoad);
+    }
+  };
+  // a wave's tiles of a piece; one that has none attends one tile without tokens
+  auto tiles_of_wave = [&](int piece) { return piece <= ws ? 0 : (piece - ws + STREAMS - 1) / STREAMS; };
+
+  int piece = lane_of(win.tiles, idx) - t0;
+  piece = piece < left ? piece : left;
+  int count = tiles_of_wave(piece);
+  int ids = pages_of(base + idx, t0, lane_of(win.len, idx), count, 0);
+  {
+    const Where at = find((t0 + ws) * kCacheTile, lane_of(win.len, idx), h, ids, 0);
+    load_k(at);
+    load_v(at);
+  }
+
+  while (true) {
+    const int b = base + idx;
+    const int n = lane_of(win.rows, idx), M = n * p.G;
+    const int len = lane_of(win.len, idx), row0 = lane_of(win.row0, idx), end = lane_of(win.end, idx);
+    const int tiles = lane_of(win.tiles, idx);
     // from here on, and again per tile and behind them, the thread's index is
     // one that the compiler has not seen: else it keeps every address of the
     // piece, the tile and the merge in a register of its own all the way
-    tx = thread;
+    int tx = thread;
     asm volatile("" : "+v"(tx));
-    const int lane = tx & 63, lr = lane & 15, lq = lane >> 4;
-    const int n = rows_of(p, b), M = n * p.G;
-    const int len = clamped_end(p, b);
-    const int row0 = p.row_start == nullptr ? b * p.max_rows : p.row_start[b];
-    const int raw_end = p.end[b];     // a causal row's last token counts from the uncut end
-    const int32_t *table = p.table + (int64_t)b * p.table_stride;
+    const int lane = tx & 63, lr = lane % NR, lq = lane / NR;
 
-    // queries: B operand of k-step s, row 16 rb + lr, the chunk of 8 channels
-    // that K's lanes hold there; from LDS (chunk c of row r at c ^ (r & 15))
-    // where they would take too many registers
-    auto chunk_of = [](int s, int lq) { return FMT == kCacheBf16 ? 4 * s + lq : FMT == kCacheMx8 ? 2 * (4 * (s >> 1) + lq) + (s & 1) : 4 * lq + s; };
-    bf16x8_t qop[4];
-    if constexpr (!AttendLds<RB>::kQueries) {
-      const int i = lr / p.G;
-      const int64_t row = row0 + i;
-      const bool ok = lr < M && row >= 0 && row < p.num_rows;
-      const uint16_t *src = p.q + (ok ? row * p.q_row_stride + (int64_t)(h * p.G + lr - i * p.G) * kCacheDim : 0);
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(src + 8 * chunk_of(s, lq));
-        qop[s] = __builtin_bit_cast(bf16x8_t, ok ? x : u32x4_t{0u, 0u, 0u, 0u});
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < RB; ++e) {
-        const int r = 16 * e + (tx >> 4), c = tx & 15;
-        const int i = r / p.G;
-        const int64_t row = row0 + i;
-        const bool ok = r < M && row >= 0 && row < p.num_rows;
-        const uint16_t *src = p.q + (ok ? row * p.q_row_stride + (int64_t)(h * p.G + r - i * p.G) * kCacheDim : 0);
-        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(src + 8 * c);
-        *reinterpret_cast<u32x4_t *>(qs + r * kLdsRow + 16 * (c ^ (r & 15))) = ok ? x : u32x4_t{0u, 0u, 0u, 0u};
-      }
-      __syncthreads();
-    }
-    // tokens that each of the lane's rows sees
-    int limit[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int i = (16 * rb + lr) / p.G;
-      const int64_t last = (int64_t)raw_end - n + i + 1;
-      limit[rb] = p.causal && last < len ? (last < 0 ? 0 : (int)last) : len;
-    }
-    const int64_t first_last = (int64_t)raw_end - n + 1;
-    const int all_see = p.causal && first_last < len ? (first_last < 0 ? 0 : (int)first_last) : len;   // tokens that every row sees
-
-    float m_run[RB], l_run[RB];
-    f32x4_t acc[RB][8];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      m_run[rb] = kNegInf;
-      l_run[rb] = 0.f;
-#pragma unroll
-      for (int db = 0; db < 8; ++db) acc[rb][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // page of half tile j of this wave's tiles: one load for 32 tiles, lane j
-    // for half tile j; -1 for what is no page
-    const int mine = (piece - w + kWaves - 1) / kWaves;     // this wave's tiles (may be 0 or less)
-    auto pages_of = [&](int k0) {
-      const int k = k0 + (lane >> 1);
-      const int64_t tok = (int64_t)(t0 + w + kWaves * k) * kCacheTile + 16 * (lane & 1);
-      int id = -1;
-      if (k < mine && tok < len) id = table[tok >> p.page_shift];
-      return id >= 0 && id < p.num_pages ? id : -1;
+    // queries: B operand of k-step s, row lr, the chunk of 8 channels that K's lanes hold there
+    auto chunk_of = [](int s, int lq) { return kPer * (kGroups * (s / kPer) + lq) + s % kPer; };
+    auto query = [&](int r, int chunk) {
+      const int i = (int)((uint32_t)r * p.g_inv >> 16);      // r / G
+      const int64_t row = (int64_t)row0 + i;
+      const bool ok = r < M && row >= 0 && row < p.num_rows;
+      const uint16_t *src = p.q + (ok ? row * p.q_row_stride + (int64_t)(h * p.G + r - i * p.G) * kCacheDim : 0);
+      const u32x4_t x = *reinterpret_cast<const u32x4_t *>(src + 8 * chunk);
+      return ok ? x : u32x4_t{0u, 0u, 0u, 0u};
     };
-    int ids = pages_of(0), ids_next = -1;
+    bf16x8_t qop[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) qop[s] = __builtin_bit_cast(bf16x8_t, query(NR * half + lr, chunk_of(s, lq)));
+    // tokens that the lane's row sees, and that every row sees
+    const int64_t last = (int64_t)end - n + 1 + (int)((uint32_t)(NR * half + lr) * p.g_inv >> 16);
+    const int limit = p.causal && last < len ? (last < 0 ? 0 : (int)last) : len;
+    const int64_t first_last = (int64_t)end - n + 1;
+    const int all_see = p.causal && first_last < len ? (first_last < 0 ? 0 : (int)first_last) : len;
 
-    Tile<FMT> cur;
-    uint32_t gone = 0;     // halves of the loaded tile without a page
-    auto load = [&](int k, Tile<FMT> &d) {
-      const int tok = (t0 + w + kWaves * k) * kCacheTile;
-      __amdgpu_buffer_rsrc_t krs[2], vrs[2], srs[2];
-      uint32_t slot[2];
-      gone = 0;
+    float m_run = kNegInf, l_run = 0.f;
+    Acc acc[kAccs];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int id = __builtin_amdgcn_readlane(ids, 2 * (k & 31) + u);
-        const int tu = tok + 16 * u;
-        int ok = len - tu;
-        ok = ok < 0 || id < 0 ? 0 : ok > 16 ? 16 : ok;
-        gone |= (id < 0 ? 1u : 0u) << u;
-        slot[u] = (uint32_t)(tu & (page_tokens - 1));
-        uint8_t *base = p.pages + (uint64_t)(id < 0 ? 0 : id) * p.page_stride + (uint64_t)h * p.head_bytes;
-        krs[u] = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, ok > 0 ? (int)p.head_bytes : 0, kBufferFlags);
-        // rows past the request's tokens read zero: a weight of zero must meet no leftover NaN
-        vrs[u] = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, ok > 0 ? (int)(v_off + (slot[u] + ok) * kRow) : 0, kBufferFlags);
-        srs[u] = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, ok > 0 ? (int)(vs_off + (slot[u] + ok) * 4) : 0, kBufferFlags);
+    for (int a = 0; a < kAccs; ++a) acc[a] = Acc{};
+
+    // the share's next piece: the next request with tiles, all of it
+    left -= piece;
+    int n_len = 0, n_t0 = 0, n_piece = 0, n_count = 0, n_ids = -1, n_h = h;
+    if (left > 0) {
+      uint64_t more = __builtin_amdgcn_ballot_w64(win.tiles > 0) & ~((2ull << idx) - 1);
+      while (more == 0) {
+        base += 64;
+        if (base >= p.B) {
+          base = 0;
+          ++n_h;
+        }
+        win = request_at(p, base + lane);
+        more = __builtin_amdgcn_ballot_w64(win.tiles > 0);
       }
+      idx = __builtin_ctzll(more);
+      n_len = lane_of(win.len, idx);
+      n_piece = lane_of(win.tiles, idx);
+      n_piece = n_piece < left ? n_piece : left;
+      n_count = tiles_of_wave(n_piece);
+      n_ids = pages_of(base + idx, 0, n_len, n_count, 0);
+    }
+    // The scores of the tile whose K is in cur, and its V into LDS as bf16.
+    auto scores = [&](float (&x)[kScores], int lane) {
+      const int lq = lane / NR;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint32_t o = (slot[u] + lr) * kRow + 16 * lq;
+      for (int u = 0; u < Tile<FMT, NR>::kBlocks; ++u) {
+        Acc s_acc = Acc{};
 #pragma unroll
-        for (int s = 0; s < Tile<FMT>::kKLoads; ++s)
-          d.k[u][s] = __builtin_amdgcn_raw_buffer_load_b128(krs[u], o + 64 * s, 0, kStreamLoad);
-        if constexpr (FMT != kCacheBf16) d.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(krs[u], ks_off + (slot[u] + lr) * 4, 0, kStreamLoad);
-      }
-      // V: 16-byte chunks of whole rows, kLanes lanes to a row
-      constexpr int kLanes = kRow / 16, kStep = 64 / kLanes;   // rows per load: 4, 8, 16
+        for (int s = 0; s < kSteps; ++s) {
+          bf16x8_t kop;
+          const u32x4_t kw = cur.k[u][s / kPer];
+          if constexpr (FMT == kCacheBf16) {
+            kop = __builtin_bit_cast(bf16x8_t, kw);
+          } else if constexpr (FMT == kCacheMx8) {
+            const float f = scale_of((cur.ks[u] >> (8 * ((kGroups * (s / kPer) + lq) / 2))) & 0xffu);
+            const u32x2_t a = widen8(kw[2 * (s % kPer)], f), d = widen8(kw[2 * (s % kPer) + 1], f);
+            kop = __builtin_bit_cast(bf16x8_t, u32x4_t{a[0], a[1], d[0], d[1]});
+          } else {
+            const float f = scale_of((cur.ks[u] >> (8 * (kGroups * (s / kPer) + lq))) & 0xffu);
+            kop = __builtin_bit_cast(bf16x8_t, widen4(kw[s % kPer], f));
+          }
+          s_acc = Mfma<NR>::run(kop, qop[s], s_acc);
+        }
 #pragma unroll
-      for (int i = 0; i < Tile<FMT>::kVLoads; ++i) {
-        const int u = i * kStep / 16;
-        const uint32_t row = slot[u] + (i * kStep) % 16 + lane / kLanes;
-        d.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vrs[u], v_off + row * kRow + 16 * (lane % kLanes), 0, kStreamLoad);
-        if constexpr (FMT != kCacheBf16)
-          d.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(srs[u], vs_off + row * 4 + (lane % kLanes) * 4 / kLanes, 0, kStreamLoad);
+        for (int e = 0; e < kRegs; ++e) x[kRegs * u + e] = s_acc[e];
       }
     };
-
-    auto tile = [&](int k, int lane) {
-      const int lr = lane & 15, lq = lane >> 4;
-      // V's transpose read: row 4 lq + lr / 4 (+ 16), chunk 2 db + (lr & 3) / 2, half lr & 1
-      const int vrow = 4 * lq + (lr >> 2);
-      const int vrd = vrow * kLdsRow + 8 * (lr & 1);
-      const int vsw = 2 * (vrow & 7);
-      const int vc0 = (lr & 3) >> 1;
-      const int tok = (t0 + w + kWaves * k) * kCacheTile;
-      const uint32_t hole = gone;
-      // V to LDS as bf16: 16-byte chunk c of row t at c ^ 2 (t & 7)
-      constexpr int kLanes = kRow / 16, kStep = 64 / kLanes;
-      bool odd = false;      // a value that is no number, where that matters
-      const bool mixed = p.causal && tok + kCacheTile > all_see;
+    auto stage = [&](int lane) {
 #pragma unroll
-      for (int i = 0; i < Tile<FMT>::kVLoads; ++i) {
+      for (int i = 0; i < Tile<FMT, NR>::kVLoads; ++i) {
         const int t = i * kStep + lane / kLanes, c = lane % kLanes;
         unsigned char *row = vs_lds + t * kLdsRow;
-        u32x4_t x[kLdsRow / kRow];
+        u32x4_t y[kPer];
         if constexpr (FMT == kCacheBf16) {
-          x[0] = cur.v[i];
+          y[0] = cur.v[i];
         } else if constexpr (FMT == kCacheMx8) {
           const float s = scale_of(cur.vs[i]);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const u32x2_t a = widen8(cur.v[i][2 * j], s), d = widen8(cur.v[i][2 * j + 1], s);
-            x[j] = u32x4_t{a[0], a[1], d[0], d[1]};
+            y[j] = u32x4_t{a[0], a[1], d[0], d[1]};
           }
         } else {
           const float s = scale_of(cur.vs[i]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = widen4(cur.v[i][j], s);
+          for (int j = 0; j < 4; ++j) y[j] = widen4(cur.v[i][j], s);
         }
 #pragma unroll
-        for (int j = 0; j < kLdsRow / kRow; ++j)
-          *reinterpret_cast<u32x4_t *>(row + 16 * ((c * (kLdsRow / kRow) + j) ^ (2 * (t & 7)))) = x[j];
-        if (mixed) {
-#pragma unroll
-          for (int j = 0; j < kLdsRow / kRow; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              odd |= (x[j][e] & 0x7f80u) == 0x7f80u || (x[j][e] & 0x7f800000u) == 0x7f800000u;
-        }
-      }
-
-      // S^T = K Q^T
-      f32x4_t sacc[2][RB];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        bf16x8_t kop[4];
-        if constexpr (FMT == kCacheBf16) {
-#pragma unroll
-          for (int s = 0; s < 4; ++s) kop[s] = __builtin_bit_cast(bf16x8_t, cur.k[u][s]);
-        } else if constexpr (FMT == kCacheMx8) {
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            const float f = scale_of((cur.ks[u] >> (16 * (s >> 1) + 8 * (lq >> 1))) & 0xffu);
-            const u32x2_t a = widen8(cur.k[u][s >> 1][2 * (s & 1)], f), d = widen8(cur.k[u][s >> 1][2 * (s & 1) + 1], f);
-            kop[s] = __builtin_bit_cast(bf16x8_t, u32x4_t{a[0], a[1], d[0], d[1]});
-          }
-        } else {
-          const float f = scale_of((cur.ks[u] >> (8 * lq)) & 0xffu);
-#pragma unroll
-          for (int s = 0; s < 4; ++s) kop[s] = __builtin_bit_cast(bf16x8_t, widen4(cur.k[u][0][s], f));
-        }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            bf16x8_t qv;
-            if constexpr (AttendLds<RB>::kQueries)
-              qv = *reinterpret_cast<const bf16x8_t *>(qs + (16 * rb + lr) * kLdsRow + 16 * (chunk_of(s, lq) ^ lr));
-            else
-              qv = qop[s];
-            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[s], qv, x, 0, 0, 0);
-          }
-          sacc[u][rb] = x;
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      load(k + 1, cur);     // behind the last tile there are no pages: such loads touch no memory
-      __builtin_amdgcn_sched_barrier(0);
-
-      const bool masked = hole != 0 || tok + kCacheTile > all_see;
-      const int odd_first = all_see > tok ? all_see - tok : 0, odd_end = len - tok < kCacheTile ? len - tok : kCacheTile;
-      const bool apart = mixed && __builtin_amdgcn_ballot_w64(odd) != 0;
-      if (apart) {
-        // A value that is no number stands at a token that some rows see and
-        // others do not, where a weight of zero would spread it.  Such tokens'
-        // V rows (kKept at most) are set aside and cleared here, and added one
-        // by one to the rows that see them.
-        for (int t = odd_first; t < odd_end; ++t)
-          if (lane < 16) {
-            u32x4_t *row = reinterpret_cast<u32x4_t *>(vs_lds + t * kLdsRow + 16 * lane);
-            *reinterpret_cast<u32x4_t *>(vs_lds + kVTile + (t - odd_first) * kLdsRow + 16 * (lane ^ (2 * (t & 7)))) = *row;
-            *row = u32x4_t{0u, 0u, 0u, 0u};
-          }
-        asm volatile("" ::: "memory");
-      }
-      constexpr int RP = RB < 2 ? RB : 2;     // row blocks at once: what P's parts take of the registers
-#pragma unroll
-      for (int r0 = 0; r0 < RB; r0 += RP) {
-      bf16x8_t part[RP][3];
-#pragma unroll
-      for (int rp = 0; rp < RP; ++rp) {
-        const int rb = r0 + rp;
-        float x[8], mx = kNegInf;
-        if (!masked) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] = sacc[e >> 2][rb][e & 3];
-            mx = fmaxf(mx, x[e]);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int t = tok + 16 * (e >> 2) + 4 * lq + (e & 3);
-            const bool sees = t < limit[rb] && !((hole >> (e >> 2)) & 1u);
-            x[e] = sees ? sacc[e >> 2][rb][e & 3] : kNegInf;
-            mx = fmaxf(mx, x[e]);
-          }
-        }
-        mx *= p.scale_log2;
-        if (__builtin_amdgcn_ballot_w64(mx > m_run[rb] + kSlack)) {
-          const float mn = fmaxf(m_run[rb], xgroup_max(mx));
-          const float alpha = mn == kNegInf ? 1.f : exp2_fast(m_run[rb] - mn);
-          l_run[rb] *= alpha;
-#pragma unroll
-          for (int db = 0; db < 8; ++db) acc[rb][db] *= alpha;
-          m_run[rb] = mn;
-        }
-        const float ms = m_run[rb] == kNegInf ? 0.f : m_run[rb];
-        float ls = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float pe = exp2_fast(__builtin_fmaf(x[e], p.scale_log2, -ms));
-          ls += pe;
-          const __bf16 a = (__bf16)pe;
-          const float r1 = pe - (float)a;
-          const __bf16 m = (__bf16)r1;
-          part[rp][0][e] = a;
-          part[rp][1][e] = m;
-          part[rp][2][e] = (__bf16)(r1 - (float)m);
-        }
-        l_run[rb] += ls;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-
-      if (apart) {
-        for (int t = odd_first; t < odd_end; ++t) {
-          const unsigned char *row = vs_lds + kVTile + (t - odd_first) * kLdsRow + 8 * lq;
-          const int e = 4 * (t >> 4) + (t & 3);
-#pragma unroll
-          for (int rp = 0; rp < RP; ++rp) {
-            const int rb = r0 + rp;
-            float pe = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) pe = j == e ? (float)part[rp][0][j] + (float)part[rp][1][j] + (float)part[rp][2][j] : pe;
-            pe = __shfl(pe, lr + 16 * ((t >> 2) & 3));
-            if (tok + t >= limit[rb]) continue;
-#pragma unroll
-            for (int db = 0; db < 8; ++db) {
-              const u32x2_t x = *reinterpret_cast<const u32x2_t *>(row + 32 * db);
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                acc[rb][db][j] += pe * __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16);
-            }
-          }
-        }
-      }
-
-      // O^T += V^T P^T
-#pragma unroll
-      for (int db = 0; db < 8; ++db) {
-        if (db == 4) __builtin_amdgcn_sched_barrier(0);
-        const int off = vrd + 16 * ((2 * db + vc0) ^ vsw);
-        const s16x4_t v0 = lds_read_tr16(vs_lds + off);
-        const s16x4_t v1 = lds_read_tr16(vs_lds + off + 16 * kLdsRow);
-        const bf16x8_t vop = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int rp = 0; rp < RP; ++rp)
-#pragma unroll
-          for (int j = 0; j < 3; ++j)
-            acc[r0 + rp][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, part[rp][j], acc[r0 + rp][db], 0, 0, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < kPer; ++j) *reinterpret_cast<u32x4_t *>(row + 16 * ((c * kPer + j) ^ swizzle<FMT, NR>(t))) = y[j];
       }
     };
 
-    if (mine > 0) {
-      load(0, cur);
-      for (int k = 0; k < mine; ++k) {
-        if ((k & 31) == 0) ids_next = pages_of(k + 32);
-        // tile k is in flight; the loads of tile k + 1 take its pages from the next word
-        if ((k & 31) == 31) ids = ids_next;
-        int l = lane;
-        asm volatile("" : "+v"(l));
-        tile(k, l);
-      }
-    }
+    int ids_next = pages_of(b, t0, len, count, 32);
+    // Issue the loads of tile k of this piece, or of the next piece's first.
+    auto load_tile = [&](int k) {
+      const bool here = k < count;
+      const Where at = find(here ? (t0 + ws + STREAMS * k) * kCacheTile : (n_t0 + ws) * kCacheTile, here ? len : n_len, here ? h : n_h,
+                            here ? ids : n_ids, here ? 2 * (k & 31) : 0);
+      load_k(at);
+      load_v(at);
+    };
 
-    // the waves' states -> LDS, merged by kSegs threads per row
+    float x[kScores];
+    uint32_t hole = gone;      // of the tile that x belongs to
+    scores(x, lane);
+    stage(lane);
+    load_tile(1);
+
+    int k = 0;
+    do {
+      int lane = tx & 63;
+      asm volatile("" : "+v"(lane));
+      const int lr = lane % NR, lq = lane / NR;
+      const int tok = (t0 + ws + STREAMS * k) * kCacheTile;
+      const bool mixed = p.causal && tok + kCacheTile > all_see;
+      if (hole != 0 || tok + kCacheTile > all_see) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) l_run[rb] = xgroup_sum(l_run[rb]);
+        for (int e = 0; e < kScores; ++e) {
+          const int t = 4 * kGroups * (e >> 2) + 4 * lq + (e & 3);
+          x[e] = tok + t >= limit || ((hole >> (t >> 4)) & 1u) ? kNegInf : x[e];
+        }
+      }
+      float mx = kNegInf;
+#pragma unroll
+      for (int e = 0; e < kScores; ++e) mx = fmaxf(mx, x[e]);
+      mx *= p.scale_log2;
+      if (__builtin_amdgcn_ballot_w64(mx > m_run + kSlack)) {
+        const float mn = fmaxf(m_run, xgroup_max<kGroups>(mx));
+        const float alpha = mn == kNegInf ? 1.f : exp2_fast(m_run - mn);
+        l_run *= alpha;
+#pragma unroll
+        for (int a = 0; a < kAccs; ++a) acc[a] *= alpha;
+        m_run = mn;
+      }
+      const float ms = m_run == kNegInf ? 0.f : m_run;
+      if (mixed) {
+        // Values that are no numbers at tokens that some rows see and others do
+        // not: a weight of zero would spread them.  Such tokens, SS_MAX_CANDIDATES -
+        // 1 at most, are then added one by one to the rows that see them, and
+        // their V rows are cleared for the others.
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < kVTile / 1024; ++i) {
+          const u32x4_t y = *reinterpret_cast<const u32x4_t *>(vs_lds + 1024 * i + 16 * lane);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= (y[e] & 0x7f80u) == 0x7f80u || (y[e] & 0x7f800000u) == 0x7f800000u;
+        }
+        const int stop = __builtin_amdgcn_ballot_w64(odd) == 0 ? 0 : len - tok < kCacheTile ? len - tok : kCacheTile;
+        for (int t = all_see > tok ? all_see - tok : 0; t < stop; ++t) {
+          unsigned char *row = vs_lds + t * kLdsRow;
+          const int e = 4 * (t / (4 * kGroups)) + (t & 3);
+          float xe = 0.f;
+#pragma unroll
+          for (int j = 0; j < kScores; ++j) xe = j == e ? x[j] : xe;
+          xe = __shfl(xe, lr + NR * ((t >> 2) % kGroups));
+          const float pe = exp2_fast(__builtin_fmaf(xe, p.scale_log2, -ms));
+          if (tok + t < limit) {
+#pragma unroll
+            for (int c = 0; c < kChans; ++c) {
+              const int at = 4 * kGroups * c + 4 * lq;     // the piece's first channel
+              const u32x2_t y = *reinterpret_cast<const u32x2_t *>(row + 16 * ((at >> 3) ^ swizzle<FMT, NR>(t)) + 8 * (lq & 1));
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                acc[4 * c / kRegs][4 * c % kRegs + j] += pe * __uint_as_float(j & 1 ? y[j >> 1] & 0xffff0000u : y[j >> 1] << 16);
+            }
+          }
+          asm volatile("" ::: "memory");
+          if (lane < 16) *reinterpret_cast<u32x4_t *>(row + 16 * lane) = u32x4_t{0u, 0u, 0u, 0u};
+          asm volatile("" ::: "memory");
+        }
+      }
+
+      // O^T += V^T P^T.  V's transpose read for k-step t: a 16-lane group's 4 rows
+      // from 16 t + 4 lq on (and 4 kGroups further), 16 channels of the NR from
+      // NR a on; lane i of the group addresses row i / 4, 4 channels from 4 (i % 4) on.
+      // The swizzle leaves a row's 256 bytes aligned, so the accumulator's part of
+      // the address is a flip of bits.
+      const int li = lane & 15;
+      const int vrow = 4 * lq + (li >> 2), chunk = (NR == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((li & 3) >> 1);
+      const uint32_t vat = (uint32_t)(uintptr_t)vs_lds + vrow * kLdsRow + 16 * (chunk ^ swizzle<FMT, NR>(vrow)) + 8 * (li & 1);
+      bf16x8_t vop[kVSteps][kAccs];
+#pragma unroll
+      for (int t = 0; t < kVSteps; ++t)
+#pragma unroll
+        for (int a = 0; a < kAccs; ++a) {
+          const uint32_t at = (vat ^ (NR * 2 * a)) + 16 * t * kLdsRow;
+          const s16x4_t v0 = lds_read_tr16(at), v1 = lds_read_tr16(at + 4 * kGroups * kLdsRow);
+          vop[t][a] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+#pragma unroll
+      for (int t = 0; t < kVSteps; ++t) {
+        u32x4_t part[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = exp2_fast(__builtin_fmaf(x[8 * t + 2 * e], p.scale_log2, -ms));
+          const float p1 = exp2_fast(__builtin_fmaf(x[8 * t + 2 * e + 1], p.scale_log2, -ms));
+          l_run += p0;
+          l_run += p1;
+          uint32_t a, b, c;
+          cut3(p0, p1, a, b, c);
+          part[0][e] = a;
+          part[1][e] = b;
+          part[2][e] = c;
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+#pragma unroll
+          for (int a = 0; a < kAccs; ++a) acc[a] = Mfma<NR>::run(vop[t][a], __builtin_bit_cast(bf16x8_t, part[j]), acc[a]);
+      }
+      // the next tile, in the shade of these products; behind a piece's last
+      // tile this is for nothing, and its loads stay for the next piece
+      hole = gone;
+      scores(x, lane);
+      stage(lane);
+      if (++k < count) {
+        if ((k & 31) == 31) {
+          ids = ids_next;
+          ids_next = pages_of(b, t0, len, count, k + 33);
+        }
+        load_tile(k + 1);
+      }
+    } while (k < count);
+
+    l_run = xgroup_sum<kGroups>(l_run);
+    auto piece_of = [&](int c) {
+      return f32x4_t{acc[4 * c / kRegs][4 * c % kRegs], acc[4 * c / kRegs][4 * c % kRegs + 1], acc[4 * c / kRegs][4 * c % kRegs + 2],
+                     acc[4 * c / kRegs][4 * c % kRegs + 3]};
+    };
+    // Row r's state (m, l) with pieces a[k] of 4 channels, at every kSegs-th 4 channels from the seg-th on
+    auto finish = [&](int r, int seg, auto segs, float m, float l, auto piece_at) {
+      constexpr int kSegs = decltype(segs)::value, kPieces = kCacheDim / 4 / kSegs;
+      if (piece == tiles) {
+        const int i = (int)((uint32_t)r * p.g_inv >> 16);
+        const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + r - i * p.G;
+        if (row0 + i >= 0 && row0 + i < p.num_rows) {
+          const RowEnd end = row_end(p, row, m, l);
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) {
+            const int64_t o = row * kCacheDim + 4 * (seg + kSegs * k);
+            *reinterpret_cast<f32x4_t *>(p.out + o) = row_value(p, end, o, piece_at(k));
+          }
+          if (seg == 0 && p.lse != nullptr) p.lse[row] = end.lse;
+        }
+      } else {
+        // two states per worker at most: of a pair that starts before the share, and of one that ends behind it
+        const int64_t o = (int64_t)(2 * worker + (t0 == 0 ? 1 : 0)) * p.M + r;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) *reinterpret_cast<f32x4_t *>(p.part_a + o * kCacheDim + 4 * (seg + kSegs * k)) = piece_at(k);
+        if (seg == 0) *reinterpret_cast<f32x2_t *>(p.part_ml + 2 * o) = f32x2_t{m, l};
+      }
+    };
+    if constexpr (kAlone) {
+      int lx = lane;
+      asm volatile("" : "+v"(lx));
+      const int r = lx % NR;
+      if (r < M) finish(r, lx / NR, std::integral_constant<int, kGroups>{}, m_run, l_run, piece_of);
+    } else {
+    // The waves' states, first of waves 2 and 3 into those of waves 0 and 1 (of
+    // the same rows), then what is left through LDS, kSegs threads to a row.
     __syncthreads();
     tx = thread;
     asm volatile("" : "+v"(tx));
-    float *aw = reinterpret_cast<float *>(smem + AttendLds<RB>::kQ);
-    float *mw = aw + kWaves * kRows * kAwPitch;
-    float *lw = mw + kWaves * kRows;
+    float *aw = reinterpret_cast<float *>(smem);
+    float *mw = aw + 2 * NR * kAwPitch;
+    float *lw = mw + 2 * NR;
     {
-    const int lr = tx & 15, lq = (tx >> 4) & 3;
+      const int lr = tx & (NR - 1), lq = (tx & 63) / NR;
+      const int slot = (w & 1) * NR + lr;
+      float *row = aw + slot * kAwPitch + 4 * lq;
+      if (w >= 2) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      float *row = aw + (w * kRows + rb * 16 + lr) * kAwPitch + 4 * lq;
-#pragma unroll
-      for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4_t *>(row + 16 * db) = acc[rb][db];
-      if (lq == 0) {
-        mw[w * kRows + rb * 16 + lr] = m_run[rb];
-        lw[w * kRows + rb * 16 + lr] = l_run[rb];
+        for (int c = 0; c < kChans; ++c) *reinterpret_cast<f32x4_t *>(row + 4 * kGroups * c) = piece_of(c);
+        if (lq == 0) {
+          mw[slot] = m_run;
+          lw[slot] = l_run;
+        }
       }
+      __syncthreads();
+      if (w < 2) {
+        const float mo = mw[slot], top = fmaxf(m_run, mo);
+        // without a maximum both states are zero, or no number
+        const float f = top == kNegInf ? 1.f : exp2_fast(m_run - top), fo = top == kNegInf ? 1.f : exp2_fast(mo - top);
+        const float l = f * l_run + fo * lw[slot];
+#pragma unroll
+        for (int c = 0; c < kChans; ++c) {
+          f32x4_t *at = reinterpret_cast<f32x4_t *>(row + 4 * kGroups * c);
+          *at = f * piece_of(c) + fo * *at;
+        }
+        if (lq == 0) {       // the row's other lanes have read them: a wave runs in step
+          mw[slot] = top;
+          lw[slot] = l;
+        }
+      }
+      __syncthreads();
     }
-    }
-    __syncthreads();
-    constexpr int kSegs = kThreads / kRows, kPieces = kCacheDim / 4 / kSegs;   // 16, 8 or 4 threads a row
+    constexpr int kAll = NR * HALVES, kSlots = 2 / HALVES;                 // rows of the piece; states of each
+    constexpr int kSegs = kThreads / kAll, kPieces = kCacheDim / 4 / kSegs;   // 16, 8 or 4 threads a row
     const int r = tx / kSegs, seg = tx % kSegs;
     if (r < M) {
-      float mv[kWaves], top = kNegInf;
+      float mv[kSlots], top = kNegInf;
 #pragma unroll
-      for (int j = 0; j < kWaves; ++j) {
-        mv[j] = mw[j * kRows + r];
+      for (int j = 0; j < kSlots; ++j) {
+        mv[j] = mw[j * NR + r];
         top = fmaxf(top, mv[j]);
       }
-      float f[kWaves], l = 0.f;
+      float f[kSlots], l = 0.f;
 #pragma unroll
-      for (int j = 0; j < kWaves; ++j) {
-        f[j] = top == kNegInf ? 1.f : exp2_fast(mv[j] - top);   // without a maximum every state is zero, or no number
-        l += f[j] * lw[j * kRows + r];
+      for (int j = 0; j < kSlots; ++j) {
+        f[j] = top == kNegInf ? 1.f : exp2_fast(mv[j] - top);
+        l += f[j] * lw[j * NR + r];
       }
       f32x4_t a[kPieces];
 #pragma unroll
       for (int k = 0; k < kPieces; ++k) {
         a[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < kWaves; ++j)
-          a[k] += f[j] * *reinterpret_cast<const f32x4_t *>(aw + (j * kRows + r) * kAwPitch + 4 * (seg + kSegs * k));
+        for (int j = 0; j < kSlots; ++j)
+          a[k] += f[j] * *reinterpret_cast<const f32x4_t *>(aw + (j * NR + r) * kAwPitch + 4 * (seg + kSegs * k));
       }
-      if (piece == tiles) {
-        const int i = r / p.G;
-        const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + r - i * p.G;
-        if (row0 + i >= 0 && row0 + i < p.num_rows) {
-          const RowEnd end = row_end(p, row, top, l);
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k) {
-            const int64_t o = row * kCacheDim + 4 * (seg + kSegs * k);
-            *reinterpret_cast<f32x4_t *>(p.out + o) = row_value(p, end, o, a[k]);
-          }
-          if (seg == 0 && p.lse != nullptr) p.lse[row] = end.lse;
-        }
-      } else {
-        // two states per workgroup at most: of a pair that starts before the share, and of one that ends behind it
-        const int64_t o = (int64_t)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * p.M + r;
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) *reinterpret_cast<f32x4_t *>(p.part_a + o * kCacheDim + 4 * (seg + kSegs * k)) = a[k];
-        if (seg == 0) *reinterpret_cast<f32x2_t *>(p.part_ml + 2 * o) = f32x2_t{top, l};
-      }
+      finish(r, seg, std::integral_constant<int, kSegs>{}, top, l, [&](int k) { return a[k]; });
     }
-    left -= piece;
+    }
+    if (left == 0) break;
+    h = n_h;
     t0 = 0;
-    if (++b == p.B) {
-      b = 0;
-      ++h;
-    }
-    if (left > 0) __syncthreads();
+    piece = n_piece;
+    count = n_count;
+    ids = n_ids;
+    if constexpr (!kAlone) __syncthreads();
   }
 }
 
@@ -848,50 +963,63 @@ __global__ __launch_bounds__(kThreads, RB == 4 || (RB == 2 && FMT == kCacheBf16)
 // Merge the pieces' states of each (request, KV head) that more than one
 // workgroup attended, and write the rows of requests without tokens.  A half
 // wave holds a row's 128 channels; SPLIT half waves of the workgroup share a
-// row's states (8 where a pair has many), else each takes a row of its own.
+// row's states (32 or 8 where a pair may have that many), else each takes a row
+// of its own.
 // ---------------------------------------------------------------------------
 template <int SPLIT>
-__global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttendArgs p) {
-  __shared__ int wave_sums[kWaves], found;
-  constexpr int kRowsPer = 8 / SPLIT;
+__global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_kernel(CacheAttendArgs p) {
+  constexpr int kHalves = SPLIT > 8 ? SPLIT : 8, kRowsPer = kHalves / SPLIT;
   const int tx = threadIdx.x, lane = tx & 31;
   const int part = (tx >> 5) % SPLIT;
   const int b = blockIdx.x / p.Hkv, h = blockIdx.x % p.Hkv;
   const int r = blockIdx.y * kRowsPer + (tx >> 5) / SPLIT;
-  const Count cnt = count_tiles(p, tx, wave_sums);
-  if (b >= tx * cnt.per && b < (tx + 1) * cnt.per) {
-    int s = cnt.before;
-    for (int j = tx * cnt.per; j < b; ++j) s += tiles_of(p, j);
-    found = s;
+  // tiles of the requests before b, and of all, by every wave
+  int before = 0, all = 0;
+  for (int j = tx & 63; j < p.B; j += 64) {
+    const int t = request_at(p, j).tiles;
+    all += t;
+    before += j < b ? t : 0;
   }
-  __syncthreads();
-  const int tiles = tiles_of(p, b), n = rows_of(p, b);
-  const int row0 = p.row_start == nullptr ? b * p.max_rows : p.row_start[b];
-  const int i = r / p.G;
-  const bool mine = r < n * p.G && row0 + i >= 0 && row0 + i < p.num_rows;
-  const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + r - i * p.G;
+  before = lane_of(wave_scan(before), 63);
+  all = lane_of(wave_scan(all), 63);
+  const Request q = request_at(p, b);
+  const int i = (int)((uint32_t)r * p.g_inv >> 16);
+  const bool mine = r < q.rows * p.G && q.row0 + i >= 0 && q.row0 + i < p.num_rows;
+  const int64_t row = ((int64_t)q.row0 + i) * p.Hq + h * p.G + r - i * p.G;
   float m = kNegInf, l = 0.f;
   f32x4_t a = {0.f, 0.f, 0.f, 0.f};
-  if (tiles > 0) {
-    const int share = share_of(cnt.all * p.Hkv, p.wgs);
-    const int start = h * cnt.all + found;
-    const int w0 = start / share, w1 = (start + tiles - 1) / share;
+  if (q.tiles > 0) {
+    const int share = share_of(all * p.Hkv, p.workers);
+    const int start = h * all + before;
+    const int w0 = (int)((uint32_t)start / (uint32_t)share), w1 = (int)((uint32_t)(start + q.tiles - 1) / (uint32_t)share);
     if (w0 == w1) return;           // one workgroup attended all of it
-    if (mine)
-      for (int w = w0 + part; w <= w1; w += SPLIT) {
-        const int64_t o = (int64_t)(2 * w + (w == w0 ? 1 : 0)) * p.M + r;
-        const f32x2_t ml = *reinterpret_cast<const f32x2_t *>(p.part_ml + 2 * o);
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(p.part_a + o * kCacheDim + 4 * lane);
-        const float mn = fmaxf(m, ml[0]);
-        const float fa = mn == kNegInf ? 1.f : exp2_fast(m - mn), fb = mn == kNegInf ? 1.f : exp2_fast(ml[0] - mn);
-        a = fa * a + fb * x;
-        l = fa * l + fb * ml[1];
-        m = mn;
+    if (mine) {
+      constexpr int kAhead = SPLIT > 8 ? 4 : 8;     // states in flight
+      for (int w = w0 + part; w <= w1; w += kAhead * SPLIT) {
+        f32x2_t ml[kAhead];
+        f32x4_t x[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int v = w + j * SPLIT <= w1 ? w + j * SPLIT : w1;
+          const int64_t o = (int64_t)(2 * v + (v == w0 ? 1 : 0)) * p.M + r;
+          ml[j] = *reinterpret_cast<const f32x2_t *>(p.part_ml + 2 * o);
+          x[j] = *reinterpret_cast<const f32x4_t *>(p.part_a + o * kCacheDim + 4 * lane);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          if (w + j * SPLIT > w1) break;
+          const float mn = fmaxf(m, ml[j][0]);
+          const float fa = mn == kNegInf ? 1.f : exp2_fast(m - mn), fb = mn == kNegInf ? 1.f : exp2_fast(ml[j][0] - mn);
+          a = fa * a + fb * x[j];
+          l = fa * l + fb * ml[j][1];
+          m = mn;
+        }
       }
+    }
   }
   if constexpr (SPLIT > 1) {
-    __shared__ __attribute__((aligned(16))) float sa[8][kCacheDim];
-    __shared__ float sm[8], sl[8];
+    __shared__ __attribute__((aligned(16))) float sa[kHalves][kCacheDim];
+    __shared__ float sm[kHalves], sl[kHalves];
     *reinterpret_cast<f32x4_t *>(&sa[tx >> 5][4 * lane]) = a;
     if (lane == 0) {
       sm[tx >> 5] = m;
@@ -934,16 +1062,25 @@ hipError_t launch_rows(const CacheRowsArgs &p, F1 one, F4 four, hipStream_t s) {
 
 template <int FMT>
 hipError_t attend(const CacheAttendArgs &p, hipStream_t s) {
-  if (p.M <= 16)
-    hipLaunchKernelGGL((cache_attend_kernel<FMT, 1>), dim3(p.wgs), dim3(kThreads), 0, s, p);
-  else if (p.M <= 32)
-    hipLaunchKernelGGL((cache_attend_kernel<FMT, 2>), dim3(p.wgs), dim3(kThreads), 0, s, p);
-  else
-    hipLaunchKernelGGL((cache_attend_kernel<FMT, 4>), dim3(p.wgs), dim3(kThreads), 0, s, p);
+  if (p.alone) {
+    const dim3 grid((p.workers + kWaves - 1) / kWaves);
+    if (p.M <= 16)
+      hipLaunchKernelGGL((cache_attend_kernel<FMT, 16, 1, 1>), grid, dim3(kThreads), 0, s, p);
+    else
+      hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 1, 1>), grid, dim3(kThreads), 0, s, p);
+  } else if (p.M <= 16) {
+    hipLaunchKernelGGL((cache_attend_kernel<FMT, 16, 1, 4>), dim3(p.workers), dim3(kThreads), 0, s, p);
+  } else if (p.M <= 32) {
+    hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 1, 4>), dim3(p.workers), dim3(kThreads), 0, s, p);
+  } else {
+    hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 2, 2>), dim3(p.workers), dim3(kThreads), 0, s, p);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t pairs = (int64_t)p.B * p.Hkv;
-  if (pairs * 8 <= p.wgs)
+  if (pairs * 32 <= p.workers)
+    hipLaunchKernelGGL((cache_join_kernel<32>), dim3((unsigned)pairs, p.M), dim3(1024), 0, s, p);
+  else if (pairs * 8 <= p.workers)
     hipLaunchKernelGGL((cache_join_kernel<8>), dim3((unsigned)pairs, p.M), dim3(kThreads), 0, s, p);
   else
     hipLaunchKernelGGL((cache_join_kernel<1>), dim3((unsigned)pairs, (p.M + 7) / 8), dim3(kThreads), 0, s, p);
@@ -952,12 +1089,17 @@ hipError_t attend(const CacheAttendArgs &p, hipStream_t s) {
 
 }  // namespace
 
-int cache_attend_wgs(int fmt, int B, int Hkv, int capacity, int M) {
-  (void)fmt;
-  const int64_t most = M <= 32 ? 512 : 256;
-  const int64_t tiles = (int64_t)B * Hkv * ((capacity + kCacheTile - 1) / kCacheTile);
+CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M) {
+  const int waves = attend_waves(fmt, M <= 16 ? 16 : 32);      // workgroups per CU
+  const int64_t pairs = (int64_t)B * Hkv;
+  // A wave for itself where there are pairs for every wave
+  CacheSplit r;
+  r.alone = M <= 32 && pairs >= 256 * kWaves;
+  const int64_t most = 256 * waves * (r.alone ? kWaves : 1);
+  const int64_t tiles = pairs * ((capacity + kCacheTile - 1) / kCacheTile);
   const int64_t need = (tiles + kMinShare - 1) / kMinShare;
-  return (int)(need < most ? need : most);
+  r.workers = (int)(need < most ? need : most);
+  return r;
 }
 
 hipError_t launch_cache_write(const CacheRowsArgs &p, int fmt, hipStream_t s) {

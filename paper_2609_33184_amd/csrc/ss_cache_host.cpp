@@ -104,12 +104,13 @@ void fill(ss::CacheArgs *p, const ss_cache_desc *d, const void *pages, const int
 }
 
 struct AttendLayout {
-  int wgs, M;
+  int M;
+  ss::CacheSplit split;
   size_t ml, bytes;   // offset of the maxima and sums; all of it
   explicit AttendLayout(const ss_cache_desc *d) {
     M = d->max_rows * (d->num_q_heads / d->num_kv_heads);
-    wgs = ss::cache_attend_wgs(d->format, d->num_requests, d->num_kv_heads, d->table_stride * d->page_tokens, M);
-    const size_t rows = 2 * (size_t)wgs * (size_t)M;
+    split = ss::cache_attend_split(d->format, d->num_requests, d->num_kv_heads, d->table_stride * d->page_tokens, M);
+    const size_t rows = 2 * (size_t)split.workers * (size_t)M;
     ml = rows * ss::kCacheDim * sizeof(float);
     bytes = (ml + rows * 2 * sizeof(float) + 255) / 256 * 256;
   }
@@ -210,8 +211,10 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
   p.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + layout.ml);
   p.Hq = desc->num_q_heads;
   p.G = desc->num_q_heads / desc->num_kv_heads;
+  p.g_inv = (65536u + (uint32_t)p.G - 1) / (uint32_t)p.G;
   p.M = layout.M;
-  p.wgs = layout.wgs;
+  p.workers = layout.split.workers;
+  p.alone = layout.split.alone;
   p.causal = desc->causal;
   p.scale_log2 = desc->softmax_scale * 1.4426950408889634f;
   const hipError_t e = ss::launch_cache_attend(p, desc->format, stream);
