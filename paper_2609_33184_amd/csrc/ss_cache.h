@@ -49,8 +49,9 @@ struct CacheAttendArgs : CacheArgs {
   int32_t Hq, G;
   uint32_t g_inv;                       // ceil(65536 / G): r / G = r * g_inv >> 16 for r < 64, G <= 64
   int32_t M;                            // rows per KV head: max_rows * G
-  int32_t workers;                      // shares that the call's tiles are cut into
+  int32_t workers;                      // shares that the call's units are cut into
   int32_t alone;                        // a worker is a wave, not a workgroup
+  int32_t piece_units;                  // what a piece costs beside its tiles, in tiles
   int32_t causal;
   float scale_log2;                     // softmax_scale * log2(e)
 };
@@ -59,6 +60,7 @@ struct CacheAttendArgs : CacheArgs {
 struct CacheSplit {
   int workers;
   bool alone;
+  int piece_units;
 };
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
 

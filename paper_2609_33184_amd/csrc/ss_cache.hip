@@ -319,13 +319,15 @@ constexpr int kLdsRow = 256;                        // a staged V row, bf16
 constexpr int kVTile = kCacheTile * kLdsRow;
 constexpr int kAwPitch = 132;                       // floats per row of a wave's partial accumulator
 constexpr float kSlack = 8.f;                       // log2 by which weights may pass 1
-constexpr int kMinShare = 4;                        // tiles: one per wave
+constexpr int kMinShare = 4;                        // units: a tile per wave
+// What a piece costs beside its tiles, in tiles: its first loads, its merge.
+constexpr int kPieceGroup = 8, kPieceAlone = 2;
 
-// LDS: the waves' V tiles, whose place the states of two waves take at a piece's end.
+// LDS: the waves' V tiles, and where the states of two waves meet at a piece's end.
 template <int NR, int STREAMS>
 struct AttendLds {
   static constexpr int kMerge = STREAMS == 1 ? 0 : 2 * NR * (kAwPitch + 2) * 4;
-  static constexpr int kBytes = kWaves * kVTile > kMerge ? kWaves * kVTile : kMerge;
+  static constexpr int kBytes = kWaves * kVTile + kMerge;
 };
 
 // A request as the attention needs it; in a window, lane i holds request base + i.
@@ -335,8 +337,9 @@ struct Request {
   int end;       // as given: positions count from it
   int len;       // tokens that its table reaches
   int tiles;
+  int units;     // what the shares count: the tiles and the cost of a piece
 };
-__device__ __forceinline__ Request request_at(const CacheArgs &p, int b) {
+__device__ __forceinline__ Request request_at(const CacheAttendArgs &p, int b) {
   Request r;
   const int c = b < p.B ? b : p.B - 1;     // loads without a branch, so that several calls' overlap
   r.end = p.end[c];
@@ -351,7 +354,16 @@ __device__ __forceinline__ Request request_at(const CacheArgs &p, int b) {
   r.rows = b < p.B ? r.rows : 0;
   r.len = r.end < 0 ? 0 : r.end > p.capacity ? p.capacity : r.end;
   r.tiles = r.rows == 0 ? 0 : (r.len + kCacheTile - 1) / kCacheTile;
+  r.units = r.tiles == 0 ? 0 : r.tiles + p.piece_units;
   return r;
+}
+
+// x as a value that the compiler has not seen: of the thread's index, so that it
+// does not keep every address of a piece, a tile and a merge in a register of
+// its own all the way.
+__device__ __forceinline__ int hidden(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // Inclusive prefix sum over the wave's lanes.
@@ -470,23 +482,23 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   const int worker = kAlone ? blockIdx.x * kWaves + w : blockIdx.x;
 
   // This worker's share and where it starts; every wave finds it by itself.  The
-  // requests are counted 64 at a time, lane j keeping the tiles of chunk j.
-  Request win;
-  int base = 0, idx, t0, h, left, all;
+  // requests are counted 64 at a time, lane j keeping the units of chunk j.
+  Request win;            // requests base .. base + 63
+  int base = 0, idx, skip, h, left;   // the next request, its units that are not ours, its head; our units
   {
     const int lane = thread & 63;
     const int chunks = (p.B + 63) / 64;
-    int before = 0, scan;
+    int before = 0, scan, all;
     if (chunks == 1) {
       win = request_at(p, lane);
-      scan = wave_scan(win.tiles);
+      scan = wave_scan(win.units);
       all = lane_of(scan, 63);
     } else {
       int sums = 0;
       for (int j = 0; j < chunks; j += 4) {
         int t[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = request_at(p, 64 * (j + i) + lane).tiles;
+        for (int i = 0; i < 4; ++i) t[i] = request_at(p, 64 * (j + i) + lane).units;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int sum = lane_of(wave_scan(t[i]), 63);
@@ -508,26 +520,81 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
       before = owner == 0 ? 0 : lane_of(scan, owner - 1);
       base = 64 * owner;
       win = request_at(p, base + lane);
-      scan = before + wave_scan(win.tiles);
+      scan = before + wave_scan(win.units);
     }
     idx = __builtin_popcountll(__builtin_amdgcn_ballot_w64(scan <= at));
-    t0 = at - (idx == 0 ? before : lane_of(scan, idx - 1));
+    skip = at - (idx == 0 ? before : lane_of(scan, idx - 1));
   }
 
   const int page_tokens = 1 << p.page_shift;
   const uint32_t v_off = (uint32_t)(page_tokens * kRow), ks_off = 2 * v_off, vs_off = ks_off + 4u * (uint32_t)page_tokens;
   unsigned char *vs_lds = smem + w * kVTile;
 
-  // Pages of a wave's tiles of a piece: tiles k0 .. k0 + 31 after its first, t0
-  // + ws, of a request with `len` tokens; `count` tiles in all.  Lane j holds
-  // half tile j's page, -1 for what is none.
-  auto pages_of = [&](int b, int t0, int len, int count, int k0) {
-    const int lane = thread & 63;
+  // A piece: tiles t0 .. t0 + tiles - 1 of a request's `whole`, for head h.  tiles = 0: none.
+  struct Piece {
+    int b, rows, row0, end, len, whole;
+    int h, t0, tiles;
+    int count;     // this wave's tiles: t0 + ws, + STREAMS, ...
+    int ids;       // lane j: page of half tile j of them, -1 for what is none
+  };
+  // Pages of the wave's tiles k0 .. k0 + 31 of a piece.
+  auto pages_of = [&](const Piece &q, int k0) {
+    const int lane = hidden(thread & 63);
     const int k = k0 + (lane >> 1);
-    const int64_t tok = (int64_t)(t0 + ws + STREAMS * k) * kCacheTile + 16 * (lane & 1);
+    const int64_t tok = (int64_t)(q.t0 + ws + STREAMS * k) * kCacheTile + 16 * (lane & 1);
     int id = -1;
-    if (k < count && tok < len) id = p.table[(int64_t)b * p.table_stride + (tok >> p.page_shift)];
+    if (k < q.count && tok < q.len) id = p.table[(int64_t)q.b * p.table_stride + (tok >> p.page_shift)];
     return id >= 0 && id < p.num_pages ? id : -1;
+  };
+  auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  auto uniform = [&](const Piece &q) {     // the wave's, in scalar registers
+    return Piece{one(q.b), one(q.rows), one(q.row0), one(q.end), one(q.len), one(q.whole), one(q.h), one(q.t0), one(q.tiles), one(q.count), q.ids};
+  };
+  // The share's next piece.  Its units are the piece's cost, then the tiles: a
+  // share that ends within the cost leaves the tiles to the next one.
+  auto next_piece = [&]() {
+    Piece q = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1};
+    while (left > 0) {
+      const uint64_t more = idx < 64 ? __builtin_amdgcn_ballot_w64(win.units > 0) & (~0ull << idx) : 0;
+      if (more == 0) {
+        base += 64;
+        idx = 0;
+        if (base >= p.B) {
+          base = 0;
+          if (++h >= p.Hkv) left = 0;     // not reached while nobody changes the lengths under a call
+        }
+        win = request_at(p, base + hidden(thread & 63));
+        continue;
+      }
+      idx = __builtin_ctzll(more);
+      const int units = lane_of(win.units, idx), cost = p.piece_units;
+      const int take = units - skip < left ? units - skip : left;
+      const int t0 = skip > cost ? skip - cost : 0, t1 = skip + take > cost ? skip + take - cost : 0;
+      left -= take;
+      skip = 0;
+      if (t1 > t0) {
+        q.b = base + idx;
+        q.rows = lane_of(win.rows, idx);
+        q.row0 = lane_of(win.row0, idx);
+        q.end = lane_of(win.end, idx);
+        q.len = lane_of(win.len, idx);
+        q.whole = lane_of(win.tiles, idx);
+        q.h = h;
+        q.t0 = t0;
+        q.tiles = t1 - t0;
+        q.count = q.tiles <= ws ? 0 : (q.tiles - ws + STREAMS - 1) / STREAMS;
+        q.ids = pages_of(q, 0);
+        ++idx;
+        break;
+      }
+      ++idx;
+    }
+    left = one(left);
+    idx = one(idx);
+    base = one(base);
+    skip = one(skip);
+    h = one(h);
+    return uniform(q);
   };
 
   Tile<FMT, NR> cur;
@@ -559,7 +626,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   // whole lines and stream past them (64 requests in bf16: 665 us, all through
   // the caches 742; K streamed costs 64 rows in 8 bits 435 -> 530 us).
   auto load_k = [&](const Where &at) {
-    const int lane = thread & 63, lr = lane % NR, lq = lane / NR;
+    const int lane = hidden(thread & 63), lr = lane % NR, lq = lane / NR;
 #pragma unroll
     for (int u = 0; u < Tile<FMT, NR>::kBlocks; ++u) {
       if constexpr (NR == 16) {
@@ -582,7 +649,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   // Issue the loads of its V.  Rows past the request's tokens touch no memory and
   // read zero: a weight of zero must meet no leftover NaN.
   auto load_v = [&](const Where &at) {
-    const int lane = thread & 63;
+    const int lane = hidden(thread & 63);
     __amdgpu_buffer_rsrc_t vrs[2], srs[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -598,44 +665,106 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
         cur.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(srs[u], vs_off + row * 4 + (lane % kLanes) * 4 / kLanes, 0, kStreamLoad);
     }
   };
-  // a wave's tiles of a piece; one that has none attends one tile without tokens
-  auto tiles_of_wave = [&](int piece) { return piece <= ws ? 0 : (piece - ws + STREAMS - 1) / STREAMS; };
-
-  int piece = lane_of(win.tiles, idx) - t0;
-  piece = piece < left ? piece : left;
-  int count = tiles_of_wave(piece);
-  int ids = pages_of(base + idx, t0, lane_of(win.len, idx), count, 0);
-  {
-    const Where at = find((t0 + ws) * kCacheTile, lane_of(win.len, idx), h, ids, 0);
+  // Queries of a piece: B operand of k-step s, row lr, the chunk of 8 channels that K's lanes hold there
+  bf16x8_t qop[kSteps];
+  auto load_q = [&](const Piece &q) {
+    const int lane = hidden(thread & 63), r = NR * half + lane % NR, lq = lane / NR;
+    const int i = (int)((uint32_t)r * p.g_inv >> 16);      // r / G
+    const int64_t row = (int64_t)q.row0 + i;
+    const bool ok = r < q.rows * p.G && row >= 0 && row < p.num_rows;
+    const uint16_t *src = p.q + (ok ? row * p.q_row_stride + (int64_t)(q.h * p.G + r - i * p.G) * kCacheDim : 0);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const u32x4_t y = *reinterpret_cast<const u32x4_t *>(src + 8 * (kPer * (kGroups * (s / kPer) + lq) + s % kPer));
+      qop[s] = __builtin_bit_cast(bf16x8_t, ok ? y : u32x4_t{0u, 0u, 0u, 0u});
+    }
+  };
+  // The scores of the tile whose K is in cur, and its V into LDS as bf16.
+  auto scores = [&](float (&x)[kScores], int lane) {
+    const int lq = lane / NR;
+#pragma unroll
+    for (int u = 0; u < Tile<FMT, NR>::kBlocks; ++u) {
+      Acc s_acc = Acc{};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        bf16x8_t kop;
+        const u32x4_t kw = cur.k[u][s / kPer];
+        if constexpr (FMT == kCacheBf16) {
+          kop = __builtin_bit_cast(bf16x8_t, kw);
+        } else if constexpr (FMT == kCacheMx8) {
+          const float f = scale_of((cur.ks[u] >> (8 * ((kGroups * (s / kPer) + lq) / 2))) & 0xffu);
+          const u32x2_t a = widen8(kw[2 * (s % kPer)], f), d = widen8(kw[2 * (s % kPer) + 1], f);
+          kop = __builtin_bit_cast(bf16x8_t, u32x4_t{a[0], a[1], d[0], d[1]});
+        } else {
+          const float f = scale_of((cur.ks[u] >> (8 * (kGroups * (s / kPer) + lq))) & 0xffu);
+          kop = __builtin_bit_cast(bf16x8_t, widen4(kw[s % kPer], f));
+        }
+        s_acc = Mfma<NR>::run(kop, qop[s], s_acc);
+      }
+#pragma unroll
+      for (int e = 0; e < kRegs; ++e) x[kRegs * u + e] = s_acc[e];
+    }
+  };
+  auto stage = [&](int lane) {
+#pragma unroll
+    for (int i = 0; i < Tile<FMT, NR>::kVLoads; ++i) {
+      const int t = i * kStep + lane / kLanes, c = lane % kLanes;
+      unsigned char *row = vs_lds + t * kLdsRow;
+      u32x4_t y[kPer];
+      if constexpr (FMT == kCacheBf16) {
+        y[0] = cur.v[i];
+      } else if constexpr (FMT == kCacheMx8) {
+        const float s = scale_of(cur.vs[i]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const u32x2_t a = widen8(cur.v[i][2 * j], s), d = widen8(cur.v[i][2 * j + 1], s);
+          y[j] = u32x4_t{a[0], a[1], d[0], d[1]};
+        }
+      } else {
+        const float s = scale_of(cur.vs[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = widen4(cur.v[i][j], s);
+      }
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) *reinterpret_cast<u32x4_t *>(row + 16 * ((c * kPer + j) ^ swizzle<FMT, NR>(t))) = y[j];
+    }
+  };
+  // A wave without a tile in a piece attends one without tokens.
+  Piece cp = next_piece();        // attended now
+  if (cp.tiles == 0) return;
+  Piece np = next_piece();        // the one behind it
+  Piece ahead = np;               // and the one behind that
+  int ids_next = -1, ids = cp.ids;
+  // Issue the loads of tile k of this piece, or of the next piece's first with its queries.
+  auto load_tile = [&](int k) {
+    const bool here = k < cp.count;
+    if (!here && np.tiles == 0) return;
+    asm volatile("" : "+s"(k));      // or the loop keeps copies of what depends on it, 40 registers of them
+    const Where at = find((here ? cp.t0 + ws + STREAMS * k : np.t0 + ws) * kCacheTile, here ? cp.len : np.len, here ? cp.h : np.h,
+                          here ? ids : np.ids, here ? 2 * (k & 31) : 0);
+    if (!here) load_q(np);
     load_k(at);
     load_v(at);
+    if (!here) ahead = next_piece();
+  };
+  float x[kScores];
+  {
+    const Where at = find((cp.t0 + ws) * kCacheTile, cp.len, cp.h, cp.ids, 0);
+    load_q(cp);
+    load_k(at);
+    load_v(at);
+    scores(x, hidden(thread & 63));
+    stage(hidden(thread & 63));
   }
 
   while (true) {
-    const int b = base + idx;
-    const int n = lane_of(win.rows, idx), M = n * p.G;
-    const int len = lane_of(win.len, idx), row0 = lane_of(win.row0, idx), end = lane_of(win.end, idx);
-    const int tiles = lane_of(win.tiles, idx);
-    // from here on, and again per tile and behind them, the thread's index is
-    // one that the compiler has not seen: else it keeps every address of the
-    // piece, the tile and the merge in a register of its own all the way
-    int tx = thread;
-    asm volatile("" : "+v"(tx));
-    const int lane = tx & 63, lr = lane % NR, lq = lane / NR;
+    const int n = cp.rows, M = n * p.G, len = cp.len, row0 = cp.row0, end = cp.end, h = cp.h, t0 = cp.t0;
+    int tx = hidden(thread);
+    const int lane = tx & 63, lr = lane % NR;
+    uint32_t hole = gone;      // of the tile that x belongs to
+    ids_next = pages_of(cp, 32);
+    load_tile(1);
 
-    // queries: B operand of k-step s, row lr, the chunk of 8 channels that K's lanes hold there
-    auto chunk_of = [](int s, int lq) { return kPer * (kGroups * (s / kPer) + lq) + s % kPer; };
-    auto query = [&](int r, int chunk) {
-      const int i = (int)((uint32_t)r * p.g_inv >> 16);      // r / G
-      const int64_t row = (int64_t)row0 + i;
-      const bool ok = r < M && row >= 0 && row < p.num_rows;
-      const uint16_t *src = p.q + (ok ? row * p.q_row_stride + (int64_t)(h * p.G + r - i * p.G) * kCacheDim : 0);
-      const u32x4_t x = *reinterpret_cast<const u32x4_t *>(src + 8 * chunk);
-      return ok ? x : u32x4_t{0u, 0u, 0u, 0u};
-    };
-    bf16x8_t qop[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) qop[s] = __builtin_bit_cast(bf16x8_t, query(NR * half + lr, chunk_of(s, lq)));
     // tokens that the lane's row sees, and that every row sees
     const int64_t last = (int64_t)end - n + 1 + (int)((uint32_t)(NR * half + lr) * p.g_inv >> 16);
     const int limit = p.causal && last < len ? (last < 0 ? 0 : (int)last) : len;
@@ -647,98 +776,9 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
 #pragma unroll
     for (int a = 0; a < kAccs; ++a) acc[a] = Acc{};
 
-    // the share's next piece: the next request with tiles, all of it
-    left -= piece;
-    int n_len = 0, n_t0 = 0, n_piece = 0, n_count = 0, n_ids = -1, n_h = h;
-    if (left > 0) {
-      uint64_t more = __builtin_amdgcn_ballot_w64(win.tiles > 0) & ~((2ull << idx) - 1);
-      while (more == 0) {
-        base += 64;
-        if (base >= p.B) {
-          base = 0;
-          ++n_h;
-        }
-        win = request_at(p, base + lane);
-        more = __builtin_amdgcn_ballot_w64(win.tiles > 0);
-      }
-      idx = __builtin_ctzll(more);
-      n_len = lane_of(win.len, idx);
-      n_piece = lane_of(win.tiles, idx);
-      n_piece = n_piece < left ? n_piece : left;
-      n_count = tiles_of_wave(n_piece);
-      n_ids = pages_of(base + idx, 0, n_len, n_count, 0);
-    }
-    // The scores of the tile whose K is in cur, and its V into LDS as bf16.
-    auto scores = [&](float (&x)[kScores], int lane) {
-      const int lq = lane / NR;
-#pragma unroll
-      for (int u = 0; u < Tile<FMT, NR>::kBlocks; ++u) {
-        Acc s_acc = Acc{};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          bf16x8_t kop;
-          const u32x4_t kw = cur.k[u][s / kPer];
-          if constexpr (FMT == kCacheBf16) {
-            kop = __builtin_bit_cast(bf16x8_t, kw);
-          } else if constexpr (FMT == kCacheMx8) {
-            const float f = scale_of((cur.ks[u] >> (8 * ((kGroups * (s / kPer) + lq) / 2))) & 0xffu);
-            const u32x2_t a = widen8(kw[2 * (s % kPer)], f), d = widen8(kw[2 * (s % kPer) + 1], f);
-            kop = __builtin_bit_cast(bf16x8_t, u32x4_t{a[0], a[1], d[0], d[1]});
-          } else {
-            const float f = scale_of((cur.ks[u] >> (8 * (kGroups * (s / kPer) + lq))) & 0xffu);
-            kop = __builtin_bit_cast(bf16x8_t, widen4(kw[s % kPer], f));
-          }
-          s_acc = Mfma<NR>::run(kop, qop[s], s_acc);
-        }
-#pragma unroll
-        for (int e = 0; e < kRegs; ++e) x[kRegs * u + e] = s_acc[e];
-      }
-    };
-    auto stage = [&](int lane) {
-#pragma unroll
-      for (int i = 0; i < Tile<FMT, NR>::kVLoads; ++i) {
-        const int t = i * kStep + lane / kLanes, c = lane % kLanes;
-        unsigned char *row = vs_lds + t * kLdsRow;
-        u32x4_t y[kPer];
-        if constexpr (FMT == kCacheBf16) {
-          y[0] = cur.v[i];
-        } else if constexpr (FMT == kCacheMx8) {
-          const float s = scale_of(cur.vs[i]);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const u32x2_t a = widen8(cur.v[i][2 * j], s), d = widen8(cur.v[i][2 * j + 1], s);
-            y[j] = u32x4_t{a[0], a[1], d[0], d[1]};
-          }
-        } else {
-          const float s = scale_of(cur.vs[i]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] = widen4(cur.v[i][j], s);
-        }
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) *reinterpret_cast<u32x4_t *>(row + 16 * ((c * kPer + j) ^ swizzle<FMT, NR>(t))) = y[j];
-      }
-    };
-
-    int ids_next = pages_of(b, t0, len, count, 32);
-    // Issue the loads of tile k of this piece, or of the next piece's first.
-    auto load_tile = [&](int k) {
-      const bool here = k < count;
-      const Where at = find(here ? (t0 + ws + STREAMS * k) * kCacheTile : (n_t0 + ws) * kCacheTile, here ? len : n_len, here ? h : n_h,
-                            here ? ids : n_ids, here ? 2 * (k & 31) : 0);
-      load_k(at);
-      load_v(at);
-    };
-
-    float x[kScores];
-    uint32_t hole = gone;      // of the tile that x belongs to
-    scores(x, lane);
-    stage(lane);
-    load_tile(1);
-
     int k = 0;
     do {
-      int lane = tx & 63;
-      asm volatile("" : "+v"(lane));
+      const int lane = hidden(tx & 63);
       const int lr = lane % NR, lq = lane / NR;
       const int tok = (t0 + ws + STREAMS * k) * kCacheTile;
       const bool mixed = p.causal && tok + kCacheTile > all_see;
@@ -836,19 +876,18 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
 #pragma unroll
           for (int a = 0; a < kAccs; ++a) acc[a] = Mfma<NR>::run(vop[t][a], __builtin_bit_cast(bf16x8_t, part[j]), acc[a]);
       }
-      // the next tile, in the shade of these products; behind a piece's last
-      // tile this is for nothing, and its loads stay for the next piece
+      // the next tile, maybe the next piece's first, in the shade of these products
       hole = gone;
       scores(x, lane);
       stage(lane);
-      if (++k < count) {
+      if (++k < cp.count) {
         if ((k & 31) == 31) {
           ids = ids_next;
-          ids_next = pages_of(b, t0, len, count, k + 33);
+          ids_next = pages_of(cp, k + 33);
         }
         load_tile(k + 1);
       }
-    } while (k < count);
+    } while (k < cp.count);
 
     l_run = xgroup_sum<kGroups>(l_run);
     auto piece_of = [&](int c) {
@@ -858,7 +897,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     // Row r's state (m, l) with pieces a[k] of 4 channels, at every kSegs-th 4 channels from the seg-th on
     auto finish = [&](int r, int seg, auto segs, float m, float l, auto piece_at) {
       constexpr int kSegs = decltype(segs)::value, kPieces = kCacheDim / 4 / kSegs;
-      if (piece == tiles) {
+      if (cp.tiles == cp.whole) {
         const int i = (int)((uint32_t)r * p.g_inv >> 16);
         const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + r - i * p.G;
         if (row0 + i >= 0 && row0 + i < p.num_rows) {
@@ -879,17 +918,15 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
       }
     };
     if constexpr (kAlone) {
-      int lx = lane;
-      asm volatile("" : "+v"(lx));
+      const int lx = hidden(lane);
       const int r = lx % NR;
       if (r < M) finish(r, lx / NR, std::integral_constant<int, kGroups>{}, m_run, l_run, piece_of);
     } else {
     // The waves' states, first of waves 2 and 3 into those of waves 0 and 1 (of
     // the same rows), then what is left through LDS, kSegs threads to a row.
     __syncthreads();
-    tx = thread;
-    asm volatile("" : "+v"(tx));
-    float *aw = reinterpret_cast<float *>(smem);
+    tx = hidden(thread);
+    float *aw = reinterpret_cast<float *>(smem + kWaves * kVTile);
     float *mw = aw + 2 * NR * kAwPitch;
     float *lw = mw + 2 * NR;
     {
@@ -923,7 +960,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
       __syncthreads();
     }
     constexpr int kAll = NR * HALVES, kSlots = 2 / HALVES;                 // rows of the piece; states of each
-    constexpr int kSegs = kThreads / kAll, kPieces = kCacheDim / 4 / kSegs;   // 16, 8 or 4 threads a row
+    constexpr int kSegs = kThreads / kAll;   // 16, 8 or 4 threads a row
     const int r = tx / kSegs, seg = tx % kSegs;
     if (r < M) {
       float mv[kSlots], top = kNegInf;
@@ -938,24 +975,18 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
         f[j] = top == kNegInf ? 1.f : exp2_fast(mv[j] - top);
         l += f[j] * lw[j * NR + r];
       }
-      f32x4_t a[kPieces];
-#pragma unroll
-      for (int k = 0; k < kPieces; ++k) {
-        a[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < kSlots; ++j)
-          a[k] += f[j] * *reinterpret_cast<const f32x4_t *>(aw + (j * NR + r) * kAwPitch + 4 * (seg + kSegs * k));
-      }
-      finish(r, seg, std::integral_constant<int, kSegs>{}, top, l, [&](int k) { return a[k]; });
+      finish(r, seg, std::integral_constant<int, kSegs>{}, top, l, [&](int k) {
+        const float *at = aw + r * kAwPitch + 4 * (seg + kSegs * k);
+        f32x4_t a = f[0] * *reinterpret_cast<const f32x4_t *>(at);
+        if constexpr (kSlots == 2) a += f[1] * *reinterpret_cast<const f32x4_t *>(at + NR * kAwPitch);
+        return a;
+      });
     }
     }
-    if (left == 0) break;
-    h = n_h;
-    t0 = 0;
-    piece = n_piece;
-    count = n_count;
-    ids = n_ids;
-    if constexpr (!kAlone) __syncthreads();
+    if (np.tiles == 0) break;
+    cp = uniform(np);
+    np = uniform(ahead);
+    ids = cp.ids;
   }
 }
 
@@ -976,7 +1007,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   // tiles of the requests before b, and of all, by every wave
   int before = 0, all = 0;
   for (int j = tx & 63; j < p.B; j += 64) {
-    const int t = request_at(p, j).tiles;
+    const int t = request_at(p, j).units;
     all += t;
     before += j < b ? t : 0;
   }
@@ -991,7 +1022,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   if (q.tiles > 0) {
     const int share = share_of(all * p.Hkv, p.workers);
     const int start = h * all + before;
-    const int w0 = (int)((uint32_t)start / (uint32_t)share), w1 = (int)((uint32_t)(start + q.tiles - 1) / (uint32_t)share);
+    const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + q.units - 1) / (uint32_t)share);
     if (w0 == w1) return;           // one workgroup attended all of it
     if (mine) {
       constexpr int kAhead = SPLIT > 8 ? 4 : 8;     // states in flight
@@ -1032,7 +1063,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
     for (int j = 0; j < SPLIT; ++j) top = fmaxf(top, sm[(tx >> 5) + j]);
     a = f32x4_t{0.f, 0.f, 0.f, 0.f};
     l = 0.f;
-#pragma unroll
+#pragma unroll 8
     for (int j = 0; j < SPLIT; ++j) {
       const float f = top == kNegInf ? 1.f : exp2_fast(sm[(tx >> 5) + j] - top);
       l += f * sl[(tx >> 5) + j];
@@ -1092,12 +1123,12 @@ hipError_t attend(const CacheAttendArgs &p, hipStream_t s) {
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M) {
   const int waves = attend_waves(fmt, M <= 16 ? 16 : 32);      // workgroups per CU
   const int64_t pairs = (int64_t)B * Hkv;
-  // A wave for itself where there are pairs for every wave
   CacheSplit r;
   r.alone = M <= 32 && pairs >= 256 * kWaves;
+  r.piece_units = r.alone ? kPieceAlone : kPieceGroup;
   const int64_t most = 256 * waves * (r.alone ? kWaves : 1);
-  const int64_t tiles = pairs * ((capacity + kCacheTile - 1) / kCacheTile);
-  const int64_t need = (tiles + kMinShare - 1) / kMinShare;
+  const int64_t units = pairs * ((capacity + kCacheTile - 1) / kCacheTile + r.piece_units);
+  const int64_t need = (units + kMinShare - 1) / kMinShare;
   r.workers = (int)(need < most ? need : most);
   return r;
 }

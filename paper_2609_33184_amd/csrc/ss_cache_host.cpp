@@ -215,6 +215,7 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
   p.M = layout.M;
   p.workers = layout.split.workers;
   p.alone = layout.split.alone;
+  p.piece_units = layout.split.piece_units;
   p.causal = desc->causal;
   p.scale_log2 = desc->softmax_scale * 1.4426950408889634f;
   const hipError_t e = ss::launch_cache_attend(p, desc->format, stream);
