@@ -99,7 +99,7 @@ struct Place {
   bool row;        // whether t is a row of some request
 };
 
-// starts, ends: LDS, kCacheMaxRequests + 1 and kCacheMaxRequests words.
+// starts, ends: LDS, B + 1 and B words (none without row_start).
 __device__ __forceinline__ Place place_of(const CacheArgs &p, int t, int tx, int32_t *starts, int32_t *ends) {
   int b, i, n, e;
   if (p.row_start == nullptr) {
@@ -195,7 +195,8 @@ __device__ __forceinline__ void store_row(uint8_t *rows, uint8_t *scales, int sl
 
 template <int FMT, int HEADS>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs p) {
-  __shared__ int32_t starts[kCacheMaxRequests + 1], ends[kCacheMaxRequests];
+  extern __shared__ int32_t starts[];
+  int32_t *ends = starts + p.B + 1;
   const int tx = threadIdx.x, c = tx & 15;
   const int64_t t = (int64_t)blockIdx.x * kGroupRows + (tx >> 4);
   const int h0 = blockIdx.y * HEADS;
@@ -205,8 +206,8 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs p) 
   for (int j = 0; j < HEADS; ++j) {
     const int h = h0 + j < p.Hkv ? h0 + j : p.Hkv - 1;
     const int64_t at = tl * p.row_stride + h * p.head_stride + 8 * c;
-    kx[j] = *reinterpret_cast<const u32x4_t *>(p.k + at);
-    vx[j] = *reinterpret_cast<const u32x4_t *>(p.v + at);
+    kx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.k + at));
+    vx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.v + at));
   }
   const Place pl = place_of(p, (int)t, tx, starts, ends);
   if (pl.page == nullptr) return;
@@ -224,7 +225,8 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs p) 
 
 template <int FMT, int HEADS>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
-  __shared__ int32_t starts[kCacheMaxRequests + 1], ends[kCacheMaxRequests];
+  extern __shared__ int32_t starts[];
+  int32_t *ends = starts + p.B + 1;
   const int tx = threadIdx.x, c = tx & 15;
   const int64_t t = (int64_t)blockIdx.x * kGroupRows + (tx >> 4);
   const int h0 = blockIdx.y * HEADS;
@@ -277,8 +279,8 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
   for (int j = 0; j < HEADS; ++j) {
     if (h0 + j >= p.Hkv) break;
     const int64_t at = t * p.row_stride + (h0 + j) * p.head_stride + 8 * c;
-    *reinterpret_cast<u32x4_t *>(p.k + at) = x[j][0];
-    *reinterpret_cast<u32x4_t *>(p.v + at) = x[j][1];
+    __builtin_nontemporal_store(x[j][0], reinterpret_cast<u32x4_t *>(p.k + at));
+    __builtin_nontemporal_store(x[j][1], reinterpret_cast<u32x4_t *>(p.v + at));
   }
 }
 
@@ -321,7 +323,7 @@ constexpr int kAwPitch = 132;                       // floats per row of a wave'
 constexpr float kSlack = 8.f;                       // log2 by which weights may pass 1
 constexpr int kMinShare = 4;                        // units: a tile per wave
 // What a piece costs beside its tiles, in tiles: its first loads, its merge.
-constexpr int kPieceGroup = 8, kPieceAlone = 2;
+constexpr int kPieceGroup = 16, kPieceAlone = 2;
 
 // LDS: the waves' V tiles, and where the states of two waves meet at a piece's end.
 template <int NR, int STREAMS>
@@ -1084,10 +1086,11 @@ constexpr int64_t kFewRows = 1 << 14;
 template <int FMT, typename F1, typename F4>
 hipError_t launch_rows(const CacheRowsArgs &p, F1 one, F4 four, hipStream_t s) {
   const unsigned groups = (unsigned)((p.num_rows + (int64_t)kGroupRows - 1) / kGroupRows);
+  const size_t lds = p.row_start == nullptr ? 0 : (2 * (size_t)p.B + 1) * sizeof(int32_t);
   if ((int64_t)p.num_rows * p.Hkv <= kFewRows)
-    hipLaunchKernelGGL(one, dim3(groups, p.Hkv), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL(one, dim3(groups, p.Hkv), dim3(kThreads), lds, s, p);
   else
-    hipLaunchKernelGGL(four, dim3(groups, (p.Hkv + 3) / 4), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL(four, dim3(groups, (p.Hkv + 3) / 4), dim3(kThreads), lds, s, p);
   return hipGetLastError();
 }
 
