@@ -373,13 +373,14 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
 #define SS_CACHE_MXFP8 1
 #define SS_CACHE_MXFP4 2
 
-/* Most requests of one call. */
+/* Most requests of one call, and KV heads of a cache. */
 #define SS_CACHE_MAX_REQUESTS 4096
+#define SS_CACHE_MAX_KV_HEADS 512
 
 typedef struct {
   int32_t num_requests;     /* B, 1..SS_CACHE_MAX_REQUESTS                     */
   int32_t num_q_heads;      /* Hq, a multiple of Hkv (attention only)          */
-  int32_t num_kv_heads;     /* Hkv >= 1                                        */
+  int32_t num_kv_heads;     /* Hkv, 1..SS_CACHE_MAX_KV_HEADS                   */
   int32_t head_dim;         /* d; only 128 is built (else SS_ERR_UNSUPPORTED)  */
   int32_t format;           /* SS_CACHE_BF16, SS_CACHE_MXFP8 or SS_CACHE_MXFP4 */
   int32_t page_tokens;      /* tokens of a page: 16, 32, 64, 128 or 256        */

@@ -1004,8 +1004,9 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   constexpr int kHalves = SPLIT > 8 ? SPLIT : 8, kRowsPer = kHalves / SPLIT;
   const int tx = threadIdx.x, lane = tx & 31;
   const int part = (tx >> 5) % SPLIT;
-  const int b = blockIdx.x / p.Hkv, h = blockIdx.x % p.Hkv;
-  const int r = blockIdx.y * kRowsPer + (tx >> 5) / SPLIT;
+  const int b = blockIdx.x;
+  const int item = blockIdx.y * kRowsPer + (tx >> 5) / SPLIT;     // of the request's heads and rows
+  const int h = item / p.M, r = item - h * p.M;
   // tiles of the requests before b, and of all, by every wave
   int before = 0, all = 0;
   for (int j = tx & 63; j < p.B; j += 64) {
@@ -1017,7 +1018,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   all = lane_of(wave_scan(all), 63);
   const Request q = request_at(p, b);
   const int i = (int)((uint32_t)r * p.g_inv >> 16);
-  const bool mine = r < q.rows * p.G && q.row0 + i >= 0 && q.row0 + i < p.num_rows;
+  bool mine = h < p.Hkv && r < q.rows * p.G && q.row0 + i >= 0 && q.row0 + i < p.num_rows;
   const int64_t row = ((int64_t)q.row0 + i) * p.Hq + h * p.G + r - i * p.G;
   float m = kNegInf, l = 0.f;
   f32x4_t a = {0.f, 0.f, 0.f, 0.f};
@@ -1025,7 +1026,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
     const int share = share_of(all * p.Hkv, p.workers);
     const int start = h * all + before;
     const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + q.units - 1) / (uint32_t)share);
-    if (w0 == w1) return;           // one workgroup attended all of it
+    mine &= w0 != w1;               // else one worker attended all of it
     if (mine) {
       constexpr int kAhead = SPLIT > 8 ? 4 : 8;     // states in flight
       for (int w = w0 + part; w <= w1; w += kAhead * SPLIT) {
@@ -1113,11 +1114,11 @@ hipError_t attend(const CacheAttendArgs &p, hipStream_t s) {
   if (e != hipSuccess) return e;
   const int64_t pairs = (int64_t)p.B * p.Hkv;
   if (pairs * 32 <= p.workers)
-    hipLaunchKernelGGL((cache_join_kernel<32>), dim3((unsigned)pairs, p.M), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL((cache_join_kernel<32>), dim3(p.B, p.Hkv * p.M), dim3(1024), 0, s, p);
   else if (pairs * 8 <= p.workers)
-    hipLaunchKernelGGL((cache_join_kernel<8>), dim3((unsigned)pairs, p.M), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_join_kernel<8>), dim3(p.B, p.Hkv * p.M), dim3(kThreads), 0, s, p);
   else
-    hipLaunchKernelGGL((cache_join_kernel<1>), dim3((unsigned)pairs, (p.M + 7) / 8), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_join_kernel<1>), dim3(p.B, (p.Hkv * p.M + 7) / 8), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 

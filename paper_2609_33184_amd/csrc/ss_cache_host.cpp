@@ -21,7 +21,8 @@ ss_status check_desc(const ss_cache_desc *d) {
   if (d->num_requests > SS_CACHE_MAX_REQUESTS)
     return fail(SS_ERR_UNSUPPORTED, "num_requests %d > %d", d->num_requests, SS_CACHE_MAX_REQUESTS);
   if (d->num_kv_heads < 1) return fail(SS_ERR_INVALID_ARGUMENT, "num_kv_heads must be >= 1 (got %d)", d->num_kv_heads);
-  if (d->num_kv_heads > 65535) return fail(SS_ERR_UNSUPPORTED, "num_kv_heads %d > 65535", d->num_kv_heads);
+  if (d->num_kv_heads > SS_CACHE_MAX_KV_HEADS)
+    return fail(SS_ERR_UNSUPPORTED, "num_kv_heads %d > %d", d->num_kv_heads, SS_CACHE_MAX_KV_HEADS);
   if (d->head_dim != ss::kCacheDim) return fail(SS_ERR_UNSUPPORTED, "head_dim %d is not built (only 128)", d->head_dim);
   if (d->format < SS_CACHE_BF16 || d->format > SS_CACHE_MXFP4)
     return fail(SS_ERR_INVALID_ARGUMENT, "format %d is none of the cache formats", d->format);
