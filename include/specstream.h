@@ -358,8 +358,9 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
  *     at slot t % page_tokens.  A page may serve several requests that only read
  *     it (a shared prefix); two rows written to one place race.
  *   - page_table, row_start and end are device arrays, read when the call's
- *     kernels run: a captured call follows them from replay to replay.  What
- *     they hold is checked there, not reported: a token whose page number is not
+ *     kernels run (they stay unchanged until its work has completed): a captured
+ *     call follows them from replay to replay.  What they hold is checked there,
+ *     not reported: a token whose page number is not
  *     in [0, num_pages), or whose position is negative or behind the table, is
  *     not written, reads as zeros and is not seen by the attention.  row_start
  *     ascends; rows outside [0, num_rows) are never touched.

@@ -100,13 +100,14 @@ struct Place {
 };
 
 // starts, ends: LDS, B + 1 and B words (none without row_start).
-__device__ __forceinline__ Place place_of(const CacheArgs &p, int t, int tx, int32_t *starts, int32_t *ends) {
-  int b, i, n, e;
+__device__ __forceinline__ Place place_of(const CacheArgs &p, int64_t t, int tx, int32_t *starts, int32_t *ends) {
+  int b, e;
+  int64_t i, n;
   if (p.row_start == nullptr) {
-    b = t / p.max_rows;
-    i = t - b * p.max_rows;
-    n = p.max_rows;
     if (t >= p.num_rows) return {nullptr, 0, false};
+    b = (int)((uint32_t)t / (uint32_t)p.max_rows);
+    i = t - (int64_t)b * p.max_rows;
+    n = p.max_rows;
     e = p.end[b];
   } else {
     for (int j = tx; j <= p.B; j += kThreads) {
@@ -126,11 +127,11 @@ __device__ __forceinline__ Place place_of(const CacheArgs &p, int t, int tx, int
     }
     b = lo;
     i = t - starts[b];
-    n = starts[b + 1] - starts[b];
+    n = (int64_t)starts[b + 1] - starts[b];
     if (t >= p.num_rows || i < 0 || i >= n) return {nullptr, 0, false};
     e = ends[b];
   }
-  const int64_t pos = (int64_t)e - n + i;
+  const int64_t pos = e - n + i;
   if (pos < 0 || pos >= p.capacity) return {nullptr, 0, true};
   const int page = p.table[(int64_t)b * p.table_stride + (pos >> p.page_shift)];
   if (page < 0 || page >= p.num_pages) return {nullptr, 0, true};
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs p) 
     kx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.k + at));
     vx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.v + at));
   }
-  const Place pl = place_of(p, (int)t, tx, starts, ends);
+  const Place pl = place_of(p, t, tx, starts, ends);
   if (pl.page == nullptr) return;
   constexpr int kRow = cache_row_bytes(FMT);
   const int tokens = 1 << p.page_shift;
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
   const int tx = threadIdx.x, c = tx & 15;
   const int64_t t = (int64_t)blockIdx.x * kGroupRows + (tx >> 4);
   const int h0 = blockIdx.y * HEADS;
-  const Place pl = place_of(p, (int)t, tx, starts, ends);
+  const Place pl = place_of(p, t, tx, starts, ends);
   if (!pl.row) return;
   constexpr int kRow = cache_row_bytes(FMT);
   const int tokens = 1 << p.page_shift;

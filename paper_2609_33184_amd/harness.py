@@ -269,7 +269,9 @@ class PagedCache:
     """A paged cache with its table and free pages, for a Cohort's requests.
 
     ``end[b]`` counts request b's tokens on the device, ``tokens[b]`` on the
-    host, so that ``grow`` can hand out pages without waiting for the GPU."""
+    host, so that ``grow`` can hand out pages without waiting for the GPU.  The
+    table and ``end`` change on torch's current stream: the calls' stream is that
+    one or waits for it."""
 
     def __init__(self, num_requests: int, num_q_heads: int, num_kv_heads: int, max_tokens: int, fmt: int = ss.SS_CACHE_MXFP8,
                  page_tokens: int = 64, num_pages: Optional[int] = None, max_rows: int = 1,
@@ -292,12 +294,13 @@ class PagedCache:
 
     def grow(self, rows: Sequence[int]) -> None:
         """Room for rows[b] more tokens of each request; ``end`` then counts them."""
+        need = [-(-(self.tokens[b] + n) // self.desc.page_tokens) for b, n in enumerate(rows)]
+        more = [max(0, k - len(self.owned[b])) for b, k in enumerate(need)]
+        if max(need) > self.table.shape[1] or sum(more) > len(self.free):
+            raise MemoryError("the cache is full")
         for b, n in enumerate(rows):
             self.tokens[b] += n
-            need = -(-self.tokens[b] // self.desc.page_tokens)
-            if need > self.table.shape[1] or need - len(self.owned[b]) > len(self.free):
-                raise MemoryError("the cache is full")
-            new = [self.free.pop() for _ in range(need - len(self.owned[b]))]
+            new = [self.free.pop() for _ in range(more[b])]
             if new:
                 at = len(self.owned[b])
                 self.table[b, at:at + len(new)] = torch.tensor(new, dtype=torch.int32, device=self.table.device)

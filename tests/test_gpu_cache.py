@@ -276,7 +276,7 @@ class Rows:
         return self
 
 
-HEADS = [(1, 1, 1), (8, 2, 5), (32, 8, 6), (8, 8, 1), (24, 4, 8), (64, 8, 8), (48, 8, 5), (16, 1, 1), (17, 1, 3), (64, 1, 1)]
+HEADS = [(1, 1, 1), (9, 3, 5), (15, 5, 2), (8, 2, 5), (32, 8, 6), (8, 8, 1), (24, 4, 8), (64, 8, 8), (48, 8, 5), (16, 1, 1), (17, 1, 3), (64, 1, 1)]
 
 
 @pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
@@ -327,6 +327,31 @@ def test_attend_many_requests():
     c = Cache(oc.BF16, 1, 16, end)
     c.fill_tokens(end, 3)
     Rows(c, 2, np.ones(1500, int), end).run().check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
+@pytest.mark.parametrize("B,hq,hkv,n", ((100, 8, 2, 1), (70, 8, 1, 5), (67, 16, 2, 8), (130, 32, 8, 4), (128, 48, 8, 5)))
+def test_attend_requests_by_the_hundred(fmt, B, hq, hkv, n):
+    """More requests than lanes: workgroups that share pieces and waves that work alone, up to 64 rows per KV head;
+    a long request among short and empty ones is split."""
+    rng = np.random.default_rng(B)
+    end = rng.integers(0, 70, B) * (rng.random(B) < 0.7)
+    end[B // 2], end[B - 1] = 1100, 300
+    rows = rng.integers(0, n + 1, B)
+    rows[0], rows[B // 2] = n, n
+    c = Cache(fmt, hkv, 32, end)
+    c.fill_tokens(end, 3)
+    Rows(c, hq, rows, end).run().check()
+
+
+def test_attend_shared_prefix():
+    """Two requests whose first pages are the same ones."""
+    end = [200, 170]
+    c = Cache(oc.MXFP8, 2, 32, end)
+    c.fill_tokens(end, 5)
+    c.table[1, :4] = c.table[0, :4]
+    c.dtable = _ints(c.table)
+    Rows(c, 8, [3, 2], end).run().check()
 
 
 @pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
@@ -542,6 +567,30 @@ def test_attend_repeats_and_streams():
         b.run(t)
         torch.cuda.synchronize()
         assert torch.equal(a.out, ref.out) and torch.equal(b.out, ref.out) and torch.equal(a.lse, ref.lse)
+
+
+def test_read_in_a_graph():
+    """A captured read follows the ends from replay to replay."""
+    end = [300, 220]
+    c = Cache(oc.MXFP4, 2, 32, end)
+    c.fill_tokens(end, 5)
+    e, rs = _ints([64, 40]), _ints([0, 50, 80])
+    out = torch.empty(2, 80, 2, 128, dtype=torch.bfloat16, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ss.ss_cache_read(c.desc(), *c.at(), out[0].data_ptr(), out[1].data_ptr(), 80, e.data_ptr(), rs.data_ptr(),
+                         stream=torch.cuda.current_stream().cuda_stream)
+    for _ in range(4):
+        e += 45
+        out.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        for b, n in enumerate((50, 30)):
+            upto = int(e[b])
+            k, v, _ = oc.tokens(c.pages, oc.MXFP4, 32, c.table, b, upto)
+            for got, want in ((out[0], k), (out[1], v)):
+                got = got[[0, 50][b]:[50, 80][b]].float().cpu().numpy()
+                assert np.array_equal(got, want[:, upto - n:].transpose(1, 0, 2).astype(np.float32))
 
 
 def test_step_in_a_graph():
