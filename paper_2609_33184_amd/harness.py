@@ -292,8 +292,13 @@ class PagedCache:
         self.owned: List[List[int]] = [[] for _ in range(num_requests)]
         self.free = list(range(pages))[::-1]
 
+    def _counts(self, rows: Sequence[int]) -> None:
+        if len(rows) != len(self.tokens) or min(rows) < 0:
+            raise ValueError(f"one count of tokens, 0 or more, for each of {len(self.tokens)} requests (got {list(rows)})")
+
     def grow(self, rows: Sequence[int]) -> None:
         """Room for rows[b] more tokens of each request; ``end`` then counts them."""
+        self._counts(rows)
         need = [-(-(self.tokens[b] + n) // self.desc.page_tokens) for b, n in enumerate(rows)]
         more = [max(0, k - len(self.owned[b])) for b, k in enumerate(need)]
         if max(need) > self.table.shape[1] or sum(more) > len(self.free):
@@ -309,6 +314,9 @@ class PagedCache:
 
     def release(self, rows: Sequence[int]) -> None:
         """The last rows[b] tokens of each request are rejected: their pages go back."""
+        self._counts(rows)
+        if any(n > t for n, t in zip(rows, self.tokens)):
+            raise ValueError(f"a request holds fewer tokens than it is to release (holds {self.tokens}, releases {list(rows)})")
         for b, n in enumerate(rows):
             self.tokens[b] -= n
             keep = -(-self.tokens[b] // self.desc.page_tokens)
@@ -319,10 +327,28 @@ class PagedCache:
     def _starts(self, row_start: Optional[torch.Tensor]) -> Optional[int]:
         return None if row_start is None else row_start.data_ptr()
 
+    def _row_stride(self, x: torch.Tensor, heads: int) -> int:
+        """Elements between the rows [T, heads, 128] of x; 0 (packed) where only one row or none makes it moot."""
+        d = self.desc.head_dim
+        if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != d:
+            raise ValueError(f"rows are bf16 [T, {heads}, {d}] (got {x.dtype} {list(x.shape)})")
+        if x.shape[0] == 0:
+            return 0
+        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
+            raise ValueError(f"a row's {heads} heads of {d} channels lie in one piece (got strides {x.stride()})")
+        if x.shape[0] == 1:
+            return 0
+        if x.stride(0) == 0:
+            raise ValueError("rows are not broadcast: an expanded tensor has one row in memory")
+        return x.stride(0)
+
     def write(self, k: torch.Tensor, v: torch.Tensor, stream: int, row_start: Optional[torch.Tensor] = None) -> None:
         """Rows [T, Hkv, 128] of k and v (views of one projection may be strided alike) enter the cache."""
+        stride = self._row_stride(k, self.desc.num_kv_heads)
+        if v.shape != k.shape or self._row_stride(v, self.desc.num_kv_heads) != stride:
+            raise ValueError(f"k and v have one shape and one row stride (got {list(k.shape)} {k.stride()}, {list(v.shape)} {v.stride()})")
         ss.ss_cache_write(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), k.shape[0],
-                          self.end.data_ptr(), self._starts(row_start), k.stride(0), stream)
+                          self.end.data_ptr(), self._starts(row_start), stride, stream)
 
     def read(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, stream: int, row_start: Optional[torch.Tensor] = None,
              kv_layout: int = ss.SS_KV_TOKEN_MAJOR, end: Optional[torch.Tensor] = None) -> None:
@@ -334,8 +360,12 @@ class PagedCache:
     def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
                row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
         """out, lse of rows q [T, Hq, 128], joined with ``prev``'s if given."""
+        stride = self._row_stride(q, self.desc.num_q_heads)
+        for x, shape in ((out, q.shape), (lse, q.shape[:2])) + (((prev[0], q.shape), (prev[1], q.shape[:2])) if prev else ()):
+            if x is not None and (x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous()):
+                raise ValueError(f"out, lse and prev are packed fp32 {list(q.shape)}, {list(q.shape[:2])} (got {x.dtype} {list(x.shape)})")
         ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
                            self.end.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
                            self._starts(row_start), None if prev is None else prev[0].data_ptr(),
                            None if prev is None else prev[1].data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
-                           q.stride(0), stream)
+                           stride, stream)
