@@ -1,6 +1,7 @@
 /*
  * specstream.h -- C ABI of the chunk-streamed speculative-verification
- * attention library (libspecstream.so, gfx950 / MI355X).
+ * attention library (libspecstream.so, gfx950 / MI355X), with the paged cache
+ * that holds K and V between rounds.
  *
  * What it computes (paper Sec. 4.2, "KV Streaming for Multi-Query
  * Verification"): in one verification round every request b of a Cohort has
@@ -368,8 +369,9 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
  *     on different streams (attentions with a workspace each), ordered by the
  *     caller where they write or read the same pages.  The stream belongs to the
  *     current device.  Every call may be captured into a graph.
- *   - The result does not depend on how the work is split or scheduled: equal
- *     inputs give equal bits. */
+ *   - The result does not depend on how the work is scheduled: equal calls give
+ *     equal bits.  How the attention splits its work follows from all the
+ *     requests' lengths, so a request's last bits may differ in other company. */
 #define SS_CACHE_BF16 0
 #define SS_CACHE_MXFP8 1
 #define SS_CACHE_MXFP4 2

@@ -18,6 +18,8 @@ Contents
     merge, initial state (-inf, 0, 0), GPU-resident masked pass, O = a/l),
     over any partition and order of the history; used for the invariance
     claims.
+``cache``
+    The paged cache: encode, decode, write, read and attend in float64.
 ``bruteforce.verify_attention_decimal``
     The same definition written out element by element in 50-digit decimal
     arithmetic, for tiny inputs.

@@ -87,8 +87,10 @@ __device__ __forceinline__ u32x4_t widen4(uint32_t w, float scale) {
 // lanes to a row's 128 channels: a lane holds 8 channels, four lanes a scaled
 // block.  Both directions are bound by memory; the rows' loads go out before
 // their places in the cache are looked up, which takes two round trips (starts
-// and ends, then the table).  Few rows take one head per workgroup, so that
-// the chip fills: see launch_rows.
+// and ends, then the table).  The bf16 rows stream past the caches, the pages do
+// not: what is written is attended next (32000 tokens with 8 heads written in 4
+// bits 43.5 us through the caches, 32 past them; 65536 tokens read from 8 bits 80
+// and 68, a copy's rate and a quarter more).
 // ---------------------------------------------------------------------------
 constexpr int kGroupRows = 16;
 
@@ -287,34 +289,50 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
 
 // ---------------------------------------------------------------------------
 // Attention.  The call's tiles of 32 tokens, of every request and KV head, head
-// by head, are one sequence that is cut into equal shares, one per workgroup,
-// however long the requests are.  The lengths are device data, so every
-// workgroup finds its share itself from the ends (a prefix sum over the
-// requests).  A share's part of one (request, head) is a piece; its waves
-// attend the piece's tiles w, w + 4, ... and merge through LDS.  A piece that is
-// all of its pair writes the result; the others leave their state (m, l, a) in
-// the workspace, at most two per workgroup, and cache_join_kernel merges them.
+// by head, are one sequence that is cut into equal shares, one per worker, however
+// long the requests are.  The lengths are device data, so every worker finds its
+// share itself from the ends (a prefix sum over the requests).  A share's part of
+// one (request, head) is a piece.  A worker is a workgroup, whose waves attend a
+// piece's tiles w, w + 4, ... and merge through LDS, or, where there are (request,
+// head) pairs enough, a wave.  A piece that is all of its pair writes the result;
+// the others leave their state (m, l, a) in the workspace, at most two per worker,
+// and cache_join_kernel merges them in the workers' order.  A worker that finds
+// itself the last of a pair could do that in the same launch; the release and
+// acquire between the XCDs' caches cost far more than the second launch (256
+// short requests 100 us with fences and 28.5 with coherent accesses alone, 27
+// with two launches).
 //
 // Per tile: S^T = K Q^T, K straight from memory in the operand's layout (a lane
 // holds 16 bytes at a time of one token; the channels of a k-step are permuted
 // alike in Q); softmax with one running maximum and sum per row; O^T += V^T P^T, V
 // through LDS and its transpose read, P straight from the score registers.  Up
 // to 16 rows per KV head use v_mfma_f32_16x16x32_bf16, more v_mfma_f32_32x32x16_bf16
-// (NR rows): its matrix work keeps the SIMD from issuing other instructions for 5
-// ns of 15.4, that of the two smaller ones it replaces for 8.4 (measured beside
-// independent vector instructions).  Lane l: lr = l % NR, lq = l / NR, kGroups =
+// (NR rows), beside which more vector work fits: two waves of a SIMD take 12.0 ns
+// for one of the small products (7.7 ns by itself) with 4 independent FMAs (7.8),
+// 10.3 for half a large one with them.  Lane l: lr = l % NR, lq = l / NR, kGroups =
 // 64 / NR.  In a score tile lane (lr, lq) holds, as score e, token 4 kGroups (e / 4)
 // + 4 lq + e % 4 of row lr; in O, as piece c, channels 4 kGroups c + 4 lq .. + 3.
+// The matrix instructions that take e4m3 and e2m1 operands with their scales are
+// not used for S: their sums were off by up to 2^-12 of the sum of the products'
+// magnitudes.
 //
-// A wave has the loads of its next tile in flight while it works on one, over
+// A wave has the loads of its next tile in flight while it works on one, and
+// computes that tile's scores and stages its V beside this one's products, over
 // the end of a piece too, so that a short piece does not wait for memory.
-// Requests of more than 32 rows per KV head are attended by two waves a tile,
-// 32 rows each (HALVES): accumulators of 64 rows would leave one wave per SIMD,
-// whose matrix and vector instructions then wait for each other.
+// Requests of more than 32 rows per KV head are attended by two waves a tile, 32
+// rows each (HALVES): 64 rows in one wave leave one wave per SIMD (16 x 32768
+// tokens in 8 bits 413 us, 400 with two waves, 320 to 390 since).
+//
+// What bounds it: bf16 is read at 6.7 TB/s (64 requests of 2048 to 65536 tokens,
+// 4.5 GB: 675 us, 664 with the arithmetic taken out); 8 and 4 bits with up to 16
+// rows at 6.1 and 5.2 (16 x 32768 tokens: 181 and 111 us); with 24 to 64 rows the vector and matrix instructions, which
+// the SIMD issues one after the other (16 x 32768 tokens in 4 bits with 24 rows:
+// 155 to 185 us, 130 without its loads, 94 without its arithmetic); short requests
+// the latency of a piece's first loads and of its merge.
 //
 // Precision: P enters as three bf16 parts cut from its 24 bits, so that it is
 // exact (two parts would leave 1.7e-6 of relative error in the result, against
-// 2e-7 to 5e-7); sums and accumulators are fp32.  The running maximum moves only
+// 1e-7 to 7e-7); sums and accumulators are fp32.  The running maximum moves only
 // where a score passes it by more than 2^8, which keeps a cross-lane maximum
 // and the rescaling out of most tiles; weights up to 2^8 cost no precision.
 // ---------------------------------------------------------------------------
@@ -322,8 +340,11 @@ constexpr int kLdsRow = 256;                        // a staged V row, bf16
 constexpr int kVTile = kCacheTile * kLdsRow;
 constexpr int kAwPitch = 132;                       // floats per row of a wave's partial accumulator
 constexpr float kSlack = 8.f;                       // log2 by which weights may pass 1
-constexpr int kMinShare = 4;                        // units: a tile per wave
-// What a piece costs beside its tiles, in tiles: its first loads, its merge.
+constexpr int kMinShare = 4;                        // units: 300 tokens 7.5 us, with 8 and 12 units 7.9 and 10.4
+// What a piece costs beside its tiles, in tiles: its first loads, its merge.  A
+// workgroup's at 4, 8, 12 and 16: 24 ragged requests 22.2, 20.3, 18.9 and 19.0 us,
+// 16 chunks of 4096 tokens 34.2, 34.1, 32.5 and 32.0; a wave's at 1, 2, 3 and 4: 256
+// short requests 22.7, 20.4, 21.4 and 21.4.
 constexpr int kPieceGroup = 16, kPieceAlone = 2;
 
 // LDS: the waves' V tiles, and where the states of two waves meet at a piece's end.
@@ -462,7 +483,14 @@ __device__ __forceinline__ void cut3(float p0, float p1, uint32_t &a, uint32_t &
   c = __builtin_amdgcn_perm(__float_as_uint(s1), __float_as_uint(s0), 0x07060302u);
 }
 
-constexpr int attend_waves(int fmt, int nr) { return fmt == kCacheBf16 ? (nr == 32 ? 1 : 2) : fmt == kCacheMx8 ? 2 : nr == 32 ? 2 : 3; }   // per SIMD
+// Waves per SIMD that the registers are held to.  Up to 16 rows: 8 bits with one
+// and two 8 x 6000 tokens 29.1 and 24.7 us, 4 bits with two and three 16 x 32768
+// tokens 120 and 111; more rows: 8 and 4 bits with one and two 242 and 207, 209 and
+// 166 (24 rows).  bf16 with more rows does not fit two.
+constexpr int attend_waves(int fmt, int nr) {
+  if (nr == 32) return fmt == kCacheBf16 ? 1 : 2;
+  return fmt == kCacheMx4 ? 3 : 2;
+}
 
 template <int FMT, int NR, int HALVES, int STREAMS>
 __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_kernel(CacheAttendArgs p) {
@@ -994,11 +1022,11 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
 }
 
 // ---------------------------------------------------------------------------
-// Merge the pieces' states of each (request, KV head) that more than one
-// workgroup attended, and write the rows of requests without tokens.  A half
-// wave holds a row's 128 channels; SPLIT half waves of the workgroup share a
-// row's states (32 or 8 where a pair may have that many), else each takes a row
-// of its own.
+// Merge the pieces' states of each (request, KV head) that more than one worker
+// attended, and write the rows of requests without tokens.  A half wave holds a
+// row's 128 channels; SPLIT half waves of the workgroup share a row's states (32 or
+// 8 where a pair may have that many: 32768 tokens with 4 heads, 128 states a pair,
+// 8.8 us with 8 and 6.3 with 32), else each takes a row of its own.
 // ---------------------------------------------------------------------------
 template <int SPLIT>
 __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_kernel(CacheAttendArgs p) {
@@ -1082,7 +1110,9 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   if (lane == 0 && p.lse != nullptr) p.lse[row] = end.lse;
 }
 
-// One head per workgroup up to this many rows x heads, four above.
+// One head per workgroup up to this many rows x heads, so that the chip fills,
+// four above.  Writes of 64 x 1, 32, 64 and 128 rows with 8 heads, one and four:
+// 4.1 and 4.6 us, 4.7 and 4.9, 7.2 and 6.8, 12.9 and 10.9.
 constexpr int64_t kFewRows = 1 << 14;
 
 template <int FMT, typename F1, typename F4>
@@ -1129,6 +1159,10 @@ CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M) {
   const int waves = attend_waves(fmt, M <= 16 ? 16 : 32);      // workgroups per CU
   const int64_t pairs = (int64_t)B * Hkv;
   CacheSplit r;
+  // Waves by themselves, which merge nothing, where there are pairs for every
+  // wave: with 256 to 2048 pairs of 0 to 600 tokens in 8 bits 15.5, 16.3, 21.4 and
+  // 27.0 us, workgroups 13.9, 17.3, 24.6 and 39.5; of 500 to 4000 tokens in 4 bits
+  // with 24 rows 39.7, 52.6, 84.2 and 163, workgroups 34.7, 51.6, 86.3 and 165.
   r.alone = M <= 32 && pairs >= 256 * kWaves;
   r.piece_units = r.alone ? kPieceAlone : kPieceGroup;
   const int64_t most = 256 * waves * (r.alone ? kWaves : 1);
