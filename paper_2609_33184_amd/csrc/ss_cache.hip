@@ -325,10 +325,11 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
 //
 // What bounds it: bf16 is read at 6.7 TB/s (64 requests of 2048 to 65536 tokens,
 // 4.5 GB: 675 us, 664 with the arithmetic taken out); 8 and 4 bits with up to 16
-// rows at 6.1 and 5.2 (16 x 32768 tokens: 181 and 111 us); with 24 to 64 rows the vector and matrix instructions, which
-// the SIMD issues one after the other (16 x 32768 tokens in 4 bits with 24 rows:
-// 155 to 185 us, 130 without its loads, 94 without its arithmetic); short requests
-// the latency of a piece's first loads and of its merge.
+// rows at 6.1 and 5.2 (16 x 32768 tokens: 181 and 111 us); with 24 to 64 rows the
+// vector and matrix instructions, which the SIMD issues one after the other (16 x
+// 32768 tokens in 4 bits with 24 rows: 155 to 185 us, 130 without its loads, 94
+// without its arithmetic); short requests the latency of a piece's first loads and
+// of its merge.
 //
 // Precision: P enters as three bf16 parts cut from its 24 bits, so that it is
 // exact (two parts would leave 1.7e-6 of relative error in the result, against
