@@ -431,9 +431,10 @@ size_t ss_cache_attend_workspace_bytes(const ss_cache_desc *desc);
  * prev_out, prev_lse: both null, or an earlier part's out and lse over other
  * keys (a round's, or this call's over an earlier chunk of pages); the result is
  * then of both parts' keys together (Eq. 14).  A part whose lse is -inf does not
- * count.  They may be out and lse themselves.  workspace: device, 256-byte
- * aligned, at least ss_cache_attend_workspace_bytes(desc), the call's own until
- * its work has completed; its contents do not matter. */
+ * count, whatever its values; every other one does, and a NaN of its lse or values
+ * is one of the result.  They may be out and lse themselves.  workspace: device,
+ * 256-byte aligned, at least ss_cache_attend_workspace_bytes(desc), the call's own
+ * until its work has completed; its contents do not matter. */
 ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const void *q,
                           int64_t q_row_stride, int32_t num_rows, const int32_t *row_start, const int32_t *end,
                           float *out, float *lse, const float *prev_out, const float *prev_lse, void *workspace,

@@ -411,19 +411,23 @@ __device__ __forceinline__ int share_of(int total, int wgs) {
 // The result of one row: (m, l) of its state in the log2 domain, a / l and what came before it.
 struct RowEnd {
   float inv, lse, own, prev;   // 1 / l; of all; weights of this and of the earlier part
+  bool counts, before;         // whether this and the earlier part count: all do whose lse is not -inf, NaN among them
 };
 __device__ __forceinline__ RowEnd row_end(const CacheAttendArgs &p, int64_t row, float m, float l) {
   RowEnd r;
   r.inv = l == 0.f ? 0.f : 1.f / l;
   r.lse = l == 0.f ? kNegInf : __builtin_fmaf(m, 0.69314718055994531f, logf(l));
-  r.own = 1.f;
-  r.prev = 0.f;
+  r.own = r.prev = 1.f;
+  r.counts = true;
+  r.before = false;
   if (p.prev_lse != nullptr) {
     const float q = p.prev_lse[row];
-    const float top = fmaxf(q, r.lse);
-    if (top == kNegInf) {        // neither part has a token
-      r.own = 0.f;
-    } else {
+    r.counts = r.lse != kNegInf;
+    r.before = q != kNegInf;
+    if (!r.counts) {
+      r.lse = q;
+    } else if (r.before) {
+      const float top = fmaxf(q, r.lse);         // of a number and a NaN the number: the NaN's weight is one
       const float a = expf(r.lse - top), b = expf(q - top);
       r.own = a / (a + b);
       r.prev = b / (a + b);
@@ -434,9 +438,9 @@ __device__ __forceinline__ RowEnd row_end(const CacheAttendArgs &p, int64_t row,
 }
 __device__ __forceinline__ f32x4_t row_value(const CacheAttendArgs &p, const RowEnd &r, int64_t at, f32x4_t a) {
   f32x4_t v = (r.inv * a) * r.own;
-  // a part without tokens does not count, whatever its values
-  if (r.own == 0.f) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  if (p.prev_lse != nullptr && r.prev != 0.f) v += r.prev * *reinterpret_cast<const f32x4_t *>(p.prev_out + at);
+  // a part that does not count may have any values; one whose weight underflows still brings a NaN
+  if (!r.counts) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (r.before) v += r.prev * *reinterpret_cast<const f32x4_t *>(p.prev_out + at);
   return v;
 }
 
