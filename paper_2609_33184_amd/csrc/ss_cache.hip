@@ -412,17 +412,17 @@ __device__ __forceinline__ int share_of(int total, int wgs) {
 struct RowEnd {
   float inv, lse, own, prev;   // 1 / l; of all; weights of this and of the earlier part
   bool counts, before;         // whether this and the earlier part count: all do whose lse is not -inf, NaN among them
+                               // (no token, or every score -inf, leaves l = 0)
 };
 __device__ __forceinline__ RowEnd row_end(const CacheAttendArgs &p, int64_t row, float m, float l) {
   RowEnd r;
-  r.inv = l == 0.f ? 0.f : 1.f / l;
-  r.lse = l == 0.f ? kNegInf : __builtin_fmaf(m, 0.69314718055994531f, logf(l));
+  r.counts = l != 0.f;
+  r.inv = r.counts ? 1.f / l : 0.f;
+  r.lse = r.counts ? __builtin_fmaf(m, 0.69314718055994531f, logf(l)) : kNegInf;
   r.own = r.prev = 1.f;
-  r.counts = true;
   r.before = false;
   if (p.prev_lse != nullptr) {
     const float q = p.prev_lse[row];
-    r.counts = r.lse != kNegInf;
     r.before = q != kNegInf;
     if (!r.counts) {
       r.lse = q;

@@ -66,3 +66,25 @@ def test_no_number_on_either_side(fmt, hq, n, B):
     c.fill_tokens(end, 5, k, v)
     rows = [n] * len(end)
     _check(Rows(c, hq, rows, end, causal=0, prev=_prev(sum(rows), hq, KINDS)).run())
+
+
+@pytest.mark.parametrize("hq,n", ((4, 3), (8, 6), (16, 8)))
+@pytest.mark.parametrize("joined", (False, True))
+def test_weights_that_are_all_zero(hq, n, joined):
+    """Every score of a row is -inf: the row is an empty one, whatever values its tokens have."""
+    end = [70, 40, 1500]
+    k, v = _normal(5, 1610, 1, 128), _normal(6, 1610, 1, 128)
+    k[:, :, 3] = 0.0
+    k[70:, :, 3] = -INF
+    v[80, 0, 7], v[700, 0, 100], v[1600, 0, 9] = NAN, INF, NAN
+    c = Cache(oc.BF16, 1, 16, end)
+    c.fill_tokens(end, 5, k, v)
+    rows = [n] * 3
+    q = _normal(21, 3 * n, hq // 2, 128)
+    q[:, :, 3] = 1.0
+    r = Rows(c, hq // 2, rows, end, causal=0, q=q, prev=_prev(3 * n, hq // 2, KINDS[:2]) if joined else None).run()
+    if joined:
+        _check(r)
+    else:
+        r.check()
+        assert (r.out[n:] == 0).all() and (r.lse[n:] == -INF).all()
