@@ -324,8 +324,16 @@ class PagedCache:
             del self.owned[b][keep:]
         self.end -= torch.tensor(list(rows), dtype=torch.int32, device=self.end.device)
 
+    def _counters(self, x: torch.Tensor, n: int, name: str) -> int:
+        """Address of an int32 array of n, which the kernels read as it lies."""
+        if not isinstance(x, torch.Tensor):
+            raise ValueError(f"{name} is a tensor (got {type(x).__name__})")
+        if x.dtype != torch.int32 or x.shape != (n,) or not x.is_contiguous() or x.device != self.end.device:
+            raise ValueError(f"{name} is a packed int32 [{n}] on {self.end.device} (got {x.dtype} {list(x.shape)} {x.stride()} on {x.device})")
+        return x.data_ptr()
+
     def _starts(self, row_start: Optional[torch.Tensor]) -> Optional[int]:
-        return None if row_start is None else row_start.data_ptr()
+        return None if row_start is None else self._counters(row_start, len(self.tokens) + 1, "row_start")
 
     def _row_stride(self, x: torch.Tensor, heads: int) -> int:
         """Elements between the rows [T, heads, 128] of x; 0 (packed) where only one row or none makes it moot."""
@@ -353,9 +361,9 @@ class PagedCache:
     def read(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, stream: int, row_start: Optional[torch.Tensor] = None,
              kv_layout: int = ss.SS_KV_TOKEN_MAJOR, end: Optional[torch.Tensor] = None) -> None:
         """The rows that end at ``end`` (the cache's own by default) leave as a bf16 chunk."""
-        end = self.end if end is None else end
+        ends = self._counters(self.end if end is None else end, len(self.tokens), "end")
         ss.ss_cache_read(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), num_rows,
-                         end.data_ptr(), self._starts(row_start), kv_layout, stream)
+                         ends, self._starts(row_start), kv_layout, stream)
 
     def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
                row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
