@@ -358,9 +358,31 @@ class PagedCache:
         ss.ss_cache_write(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), k.shape[0],
                           self.end.data_ptr(), self._starts(row_start), stride, stream)
 
+    def _chunk(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, kv_layout: int) -> None:
+        """k and v hold num_rows tokens in the given layout: packed, or the views of one chunk of K and V rows."""
+        heads, d = self.desc.num_kv_heads, self.desc.head_dim
+        need = num_rows * heads * d
+        for x in (k, v):
+            if not isinstance(x, torch.Tensor):
+                raise ValueError(f"a chunk is a tensor (got {type(x).__name__})")
+            if x.dtype != torch.bfloat16 or x.device != self.pages.device:
+                raise ValueError(f"a chunk is bf16 on {self.pages.device} (got {x.dtype} on {x.device})")
+        if kv_layout != ss.SS_KV_HEAD_MAJOR_KV:
+            fits = all(x.is_contiguous() and x.numel() >= need for x in (k, v))
+        else:
+            packed = zip(k.shape, k.stride(), (2 * d * num_rows, 2 * d, 1))
+            rows = k.shape == (heads, num_rows, d) and all(n == 1 or s == want for n, s, want in packed)
+            room = k.untyped_storage().nbytes() // BF16_BYTES - k.storage_offset()
+            fits = (k.is_contiguous() and k.numel() >= 2 * need or rows and room >= 2 * need) and v.data_ptr() == k.data_ptr() + BF16_BYTES * d
+        if not fits:
+            raise ValueError(f"a chunk holds {num_rows} rows of {heads} heads in layout {kv_layout} "
+                             f"(got {list(k.shape)} {k.stride()}, {list(v.shape)} {v.stride()})")
+
     def read(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, stream: int, row_start: Optional[torch.Tensor] = None,
              kv_layout: int = ss.SS_KV_TOKEN_MAJOR, end: Optional[torch.Tensor] = None) -> None:
-        """The rows that end at ``end`` (the cache's own by default) leave as a bf16 chunk."""
+        """The rows that end at ``end`` (the cache's own by default) leave as a bf16 chunk: into k and v, packed tensors of
+        num_rows tokens or more, or with SS_KV_HEAD_MAJOR_KV into one [heads, num_rows, 2, 128], v its second rows."""
+        self._chunk(k, v, num_rows, kv_layout)
         ends = self._counters(self.end if end is None else end, len(self.tokens), "end")
         ss.ss_cache_read(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), num_rows,
                          ends, self._starts(row_start), kv_layout, stream)

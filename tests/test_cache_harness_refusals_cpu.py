@@ -68,3 +68,39 @@ def test_ends_of_a_read(reached):
         with pytest.raises(ValueError, match="end"):
             p.read(k, k, 8, 0, start, end=bad)
     assert reached == []
+
+
+T, H_, HKV = ss.SS_KV_TOKEN_MAJOR, ss.SS_KV_HEAD_MAJOR, ss.SS_KV_HEAD_MAJOR_KV
+
+
+def test_chunks_that_a_read_accepts(reached):
+    """8 rows of 2 KV heads: a chunk of its shape, a longer staging buffer, and the interleaved layout's views."""
+    p, start = _cache(), torch.tensor([0, 4, 8], dtype=torch.int32)
+    flat = torch.zeros(2, 5000, dtype=BF)
+    both = torch.zeros(2, 8, 2, 128, dtype=BF)
+    for k, v, layout in ((torch.zeros(8, 2, 128, dtype=BF), torch.zeros(8, 2, 128, dtype=BF), T),
+                         (torch.zeros(2, 8, 128, dtype=BF), torch.zeros(2, 8, 128, dtype=BF), H_), (flat[0], flat[1], T),
+                         (both, both[:, :, 1], HKV), (both[:, :, 0], both[:, :, 1], HKV), (both.view(-1), both.view(-1)[128:], HKV)):
+        p.read(k, v, 8, 0, start, layout)
+    assert [c[1][3:5] for c in reached[-3:]] == [(both.data_ptr(), both.data_ptr() + 256)] * 3 and len(reached) == 6
+
+
+def test_chunks_that_a_read_refuses(reached):
+    p, start = _cache(), torch.tensor([0, 4, 8], dtype=torch.int32)
+    k = torch.zeros(8, 2, 128, dtype=BF)
+    both, one = torch.zeros(2, 8, 2, 128, dtype=BF), torch.zeros(1, 8, 2, 128, dtype=BF)
+    bad = [(x, layout) for layout in (T, H_) for x in (
+        k.float(), k.half(), k[:7], k[:0], torch.zeros(8, 2, 256, dtype=BF)[..., ::2], torch.zeros(8, 4, 128, dtype=BF)[:, :2], k[:1].expand(8, 2, 128),
+        torch.zeros(2, 8, 128, dtype=BF).transpose(0, 1), torch.empty(8, 2, 128, dtype=BF, device="meta"), None, k.data_ptr())]
+    pairs = [(x, k, layout) for x, layout in bad] + [(k, x, layout) for x, layout in bad]
+    pairs += [(both, both[:, :, 0], HKV), (both[:, :, 1], both[:, :, 0], HKV), (k, k, HKV), (both, both.clone()[:, :, 1], HKV),
+              (both[:, :7], both[:, :7, 1], HKV), (both[:, :7, 0], both[:, :7, 1], HKV), (one, one[:, :, 1], HKV), (both.float(), both.float()[:, :, 1], HKV),
+              (torch.zeros(8, 2, 2, 128, dtype=BF).transpose(0, 1), both[:, :, 1], HKV), (both[..., ::2], both[:, :, 1], HKV),
+              (both, None, HKV)]
+    for a, b, layout in pairs:
+        with pytest.raises(ValueError):
+            p.read(a, b, 8, 0, start, layout)
+    for rows in (9, 1 << 40):                           # more rows than the chunk holds
+        with pytest.raises(ValueError):
+            p.read(k, k.clone(), rows, 0, start)
+    assert reached == []
