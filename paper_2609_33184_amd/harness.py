@@ -340,6 +340,8 @@ class PagedCache:
         d = self.desc.head_dim
         if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != d:
             raise ValueError(f"rows are bf16 [T, {heads}, {d}] (got {x.dtype} {list(x.shape)})")
+        if x.device != self.pages.device:
+            raise ValueError(f"rows are on the cache's device, {self.pages.device} (got {x.device})")
         if x.shape[0] == 0:
             return 0
         if x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
@@ -392,8 +394,9 @@ class PagedCache:
         """out, lse of rows q [T, Hq, 128], joined with ``prev``'s if given."""
         stride = self._row_stride(q, self.desc.num_q_heads)
         for x, shape in ((out, q.shape), (lse, q.shape[:2])) + (((prev[0], q.shape), (prev[1], q.shape[:2])) if prev else ()):
-            if x is not None and (x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous()):
-                raise ValueError(f"out, lse and prev are packed fp32 {list(q.shape)}, {list(q.shape[:2])} (got {x.dtype} {list(x.shape)})")
+            if x is not None and (x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.device != q.device):
+                raise ValueError(f"out, lse and prev are packed fp32 {list(q.shape)}, {list(q.shape[:2])} on {q.device} "
+                                 f"(got {x.dtype} {list(x.shape)} on {x.device})")
         ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
                            self.end.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
                            self._starts(row_start), None if prev is None else prev[0].data_ptr(),

@@ -104,3 +104,17 @@ def test_chunks_that_a_read_refuses(reached):
         with pytest.raises(ValueError):
             p.read(k, k.clone(), rows, 0, start)
     assert reached == []
+
+
+def test_rows_on_another_device(reached):
+    p, (k, q, out, lse) = _cache(), _rows()
+    there = lambda x: torch.empty_like(x, device="meta")
+    for call in (lambda: p.write(there(k), k, 0), lambda: p.write(k, there(k), 0), lambda: p.attend(there(q), out, lse, 0),
+                 lambda: p.attend(q, there(out), lse, 0), lambda: p.attend(q, out, there(lse), 0),
+                 lambda: p.attend(q, out, lse, 0, prev=(there(out), lse)), lambda: p.attend(q, out, lse, 0, prev=(out, there(lse)))):
+        with pytest.raises(ValueError, match="meta"):
+            call()
+    assert reached == []
+    p.write(k, k, 0)
+    p.attend(q, out, None, 0, prev=(out, lse))
+    assert [c[0] for c in reached] == ["ss_cache_write", "ss_cache_attend"]
