@@ -324,6 +324,14 @@ class PagedCache:
             del self.owned[b][keep:]
         self.end -= torch.tensor(list(rows), dtype=torch.int32, device=self.end.device)
 
+    def _on_current_device(self) -> None:
+        """A call runs on the current device, wherever its addresses lead."""
+        device = self.pages.device
+        if device.type != "cuda":
+            raise ValueError("a cache on the CPU keeps its table only")
+        if torch.cuda.current_device() != device.index:
+            raise ValueError(f"the cache is on {device}, the current device is {torch.cuda.current_device()}")
+
     def _counters(self, x: torch.Tensor, n: int, name: str) -> int:
         """Address of an int32 array of n, which the kernels read as it lies."""
         if not isinstance(x, torch.Tensor):
@@ -357,8 +365,10 @@ class PagedCache:
         stride = self._row_stride(k, self.desc.num_kv_heads)
         if v.shape != k.shape or self._row_stride(v, self.desc.num_kv_heads) != stride:
             raise ValueError(f"k and v have one shape and one row stride (got {list(k.shape)} {k.stride()}, {list(v.shape)} {v.stride()})")
+        starts = self._starts(row_start)
+        self._on_current_device()
         ss.ss_cache_write(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), k.shape[0],
-                          self.end.data_ptr(), self._starts(row_start), stride, stream)
+                          self.end.data_ptr(), starts, stride, stream)
 
     def _chunk(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, kv_layout: int) -> None:
         """k and v hold num_rows tokens in the given layout: packed, or the views of one chunk of K and V rows."""
@@ -385,9 +395,10 @@ class PagedCache:
         """The rows that end at ``end`` (the cache's own by default) leave as a bf16 chunk: into k and v, packed tensors of
         num_rows tokens or more, or with SS_KV_HEAD_MAJOR_KV into one [heads, num_rows, 2, 128], v its second rows."""
         self._chunk(k, v, num_rows, kv_layout)
-        ends = self._counters(self.end if end is None else end, len(self.tokens), "end")
+        ends, starts = self._counters(self.end if end is None else end, len(self.tokens), "end"), self._starts(row_start)
+        self._on_current_device()
         ss.ss_cache_read(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), num_rows,
-                         ends, self._starts(row_start), kv_layout, stream)
+                         ends, starts, kv_layout, stream)
 
     def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
                row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
@@ -397,8 +408,10 @@ class PagedCache:
             if x is not None and (x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.device != q.device):
                 raise ValueError(f"out, lse and prev are packed fp32 {list(q.shape)}, {list(q.shape[:2])} on {q.device} "
                                  f"(got {x.dtype} {list(x.shape)} on {x.device})")
+        starts = self._starts(row_start)
+        self._on_current_device()
         ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
                            self.end.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-                           self._starts(row_start), None if prev is None else prev[0].data_ptr(),
+                           starts, None if prev is None else prev[0].data_ptr(),
                            None if prev is None else prev[1].data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
                            stride, stream)

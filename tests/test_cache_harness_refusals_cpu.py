@@ -26,6 +26,7 @@ def reached(monkeypatch):
     calls = []
     for name in ("ss_cache_write", "ss_cache_read", "ss_cache_attend"):
         monkeypatch.setattr(ss, name, lambda *a, _name=name, **kw: calls.append((_name, a)))
+    monkeypatch.setattr(H.PagedCache, "_on_current_device", lambda self: None, raising=False)
     return calls
 
 
@@ -118,3 +119,26 @@ def test_rows_on_another_device(reached):
     p.write(k, k, 0)
     p.attend(q, out, None, 0, prev=(out, lse))
     assert [c[0] for c in reached] == ["ss_cache_write", "ss_cache_attend"]
+
+
+def test_devices_without_the_cache(monkeypatch):
+    """A cache on the CPU counts pages and runs nothing; one of another GPU than the current runs nothing either."""
+    calls = []
+    for name in ("ss_cache_write", "ss_cache_read", "ss_cache_attend"):
+        monkeypatch.setattr(ss, name, lambda *a, **kw: calls.append(a))
+    p, (k, q, out, lse) = _cache(), _rows()
+    every = (lambda: p.write(k, k, 0), lambda: p.read(k, k.clone(), 8, 0), lambda: p.attend(q, out, lse, 0))
+    for call in every:
+        with pytest.raises(ValueError, match="CPU"):
+            call()
+
+    class Pages:
+        device = torch.device("cuda", 1)
+
+    p.pages = Pages()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current"):
+        p._on_current_device()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    p._on_current_device()
+    assert calls == []
