@@ -5,6 +5,7 @@ of the round runs in libspecstream's kernels through the binding.
 """
 from __future__ import annotations
 
+import operator
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -292,13 +293,15 @@ class PagedCache:
         self.owned: List[List[int]] = [[] for _ in range(num_requests)]
         self.free = list(range(pages))[::-1]
 
-    def _counts(self, rows: Sequence[int]) -> None:
+    def _counts(self, rows: Sequence[int]) -> List[int]:
+        rows = [operator.index(n) for n in rows]
         if len(rows) != len(self.tokens) or min(rows) < 0:
-            raise ValueError(f"one count of tokens, 0 or more, for each of {len(self.tokens)} requests (got {list(rows)})")
+            raise ValueError(f"one count of tokens, 0 or more, for each of {len(self.tokens)} requests (got {rows})")
+        return rows
 
     def grow(self, rows: Sequence[int]) -> None:
         """Room for rows[b] more tokens of each request; ``end`` then counts them."""
-        self._counts(rows)
+        rows = self._counts(rows)
         need = [-(-(self.tokens[b] + n) // self.desc.page_tokens) for b, n in enumerate(rows)]
         more = [max(0, k - len(self.owned[b])) for b, k in enumerate(need)]
         if max(need) > self.table.shape[1] or sum(more) > len(self.free):
@@ -310,19 +313,19 @@ class PagedCache:
                 at = len(self.owned[b])
                 self.table[b, at:at + len(new)] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
                 self.owned[b] += new
-        self.end += torch.tensor(list(rows), dtype=torch.int32, device=self.end.device)
+        self.end += torch.tensor(rows, dtype=torch.int32, device=self.end.device)
 
     def release(self, rows: Sequence[int]) -> None:
         """The last rows[b] tokens of each request are rejected: their pages go back."""
-        self._counts(rows)
+        rows = self._counts(rows)
         if any(n > t for n, t in zip(rows, self.tokens)):
-            raise ValueError(f"a request holds fewer tokens than it is to release (holds {self.tokens}, releases {list(rows)})")
+            raise ValueError(f"a request holds fewer tokens than it is to release (holds {self.tokens}, releases {rows})")
         for b, n in enumerate(rows):
             self.tokens[b] -= n
             keep = -(-self.tokens[b] // self.desc.page_tokens)
             self.free += self.owned[b][keep:]
             del self.owned[b][keep:]
-        self.end -= torch.tensor(list(rows), dtype=torch.int32, device=self.end.device)
+        self.end -= torch.tensor(rows, dtype=torch.int32, device=self.end.device)
 
     def _on_current_device(self) -> None:
         """A call runs on the current device, wherever its addresses lead."""

@@ -142,3 +142,20 @@ def test_devices_without_the_cache(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     p._on_current_device()
     assert calls == []
+
+
+def test_counts_are_whole_numbers():
+    p = H.PagedCache(2, 8, 2, 64, ss.SS_CACHE_BF16, 16, device="cpu")
+    p.grow([20, 5])
+    state = lambda: (list(p.tokens), [list(x) for x in p.owned], list(p.free), p.table.tolist(), p.end.tolist())
+    before = state()
+    for call in (p.grow, p.release):
+        for rows in ([0, 1.5], [13.0, 1], [1, "1"], [1, None], torch.tensor([1.0, 1.0])):
+            with pytest.raises(TypeError):
+                call(rows)
+            assert state() == before
+    for rows in (torch.tensor([13, 1]), (torch.tensor(13).numpy(), True)):
+        p.grow(rows)
+        assert p.tokens == [33, 6] and p.end.tolist() == [33, 6] and all(type(n) is int for n in p.tokens)
+        p.release(rows)
+        assert p.tokens == [20, 5] and p.end.tolist() == [20, 5] and [len(x) for x in p.owned] == [2, 1]
