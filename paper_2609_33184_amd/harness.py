@@ -297,7 +297,20 @@ class PagedCache:
         rows = [operator.index(n) for n in rows]
         if len(rows) != len(self.tokens) or min(rows) < 0:
             raise ValueError(f"one count of tokens, 0 or more, for each of {len(self.tokens)} requests (got {rows})")
+        if self.end.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("grow and release change the host's counts too: they cannot be captured")
         return rows
+
+    def _post(self, rows: List[int], places: List[int], ids: List[int]) -> None:
+        """``end`` and table entries change on torch's current stream.  The numbers travel in one copy from pinned
+        memory, which torch hands out again only once that copy is done, so that the host waits for nothing."""
+        x = torch.tensor(rows + places + ids, dtype=torch.int32)
+        if self.end.is_cuda:
+            x = x.pin_memory().to(self.end.device, non_blocking=True)
+        n, m = len(rows), len(rows) + len(places)
+        if ids:
+            self.table.view(-1)[x[n:m]] = x[m:]
+        self.end += x[:n]
 
     def grow(self, rows: Sequence[int]) -> None:
         """Room for rows[b] more tokens of each request; ``end`` then counts them."""
@@ -306,14 +319,15 @@ class PagedCache:
         more = [max(0, k - len(self.owned[b])) for b, k in enumerate(need)]
         if max(need) > self.table.shape[1] or sum(more) > len(self.free):
             raise MemoryError("the cache is full")
+        places, ids = [], []
         for b, n in enumerate(rows):
             self.tokens[b] += n
+            at = b * self.table.shape[1] + len(self.owned[b])
             new = [self.free.pop() for _ in range(more[b])]
-            if new:
-                at = len(self.owned[b])
-                self.table[b, at:at + len(new)] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
-                self.owned[b] += new
-        self.end += torch.tensor(rows, dtype=torch.int32, device=self.end.device)
+            self.owned[b] += new
+            places += range(at, at + len(new))
+            ids += new
+        self._post(rows, places, ids)
 
     def release(self, rows: Sequence[int]) -> None:
         """The last rows[b] tokens of each request are rejected: their pages go back."""
@@ -325,7 +339,7 @@ class PagedCache:
             keep = -(-self.tokens[b] // self.desc.page_tokens)
             self.free += self.owned[b][keep:]
             del self.owned[b][keep:]
-        self.end -= torch.tensor(rows, dtype=torch.int32, device=self.end.device)
+        self._post([-n for n in rows], [], [])
 
     def _on_current_device(self) -> None:
         """A call runs on the current device, wherever its addresses lead."""
