@@ -6,7 +6,7 @@ of the round runs in libspecstream's kernels through the binding.
 from __future__ import annotations
 
 import operator
-from typing import List, Optional, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -266,13 +266,74 @@ def run_round_single_slot(b: RoundBuffers, host: HostHistory, slot: torch.Tensor
         ss.ss_event_destroy(free)
 
 
+class _Order:
+    """Streams of a cache's calls and of the changes of its table.  A change comes after the calls before it, a call
+    after the last change, an attention after the last attention (they share a workspace); calls on the changes' own
+    stream need nothing for that."""
+
+    def __init__(self, device):
+        self.device = device
+        self.home = torch.cuda.current_stream(device)      # of the last change
+        self.changed = torch.cuda.Event()
+        self.changed.record(self.home)
+        self.calls: Dict[int, torch.cuda.Event] = {}       # since then, on other streams, by handle
+        self.attended: Optional[int] = None                # the last attention's stream, if there was one since
+
+    def change_begins(self) -> None:
+        now = torch.cuda.current_stream(self.device)
+        if now.cuda_stream != self.home.cuda_stream:
+            now.wait_stream(self.home)
+        for handle, done in self.calls.items():
+            if handle != now.cuda_stream:
+                now.wait_event(done)
+        self.home = now
+
+    def change_ends(self) -> None:
+        self.changed.record(self.home)
+        self.calls.clear()
+        self.attended = None
+
+    def call_begins(self, handle: int, attends: bool) -> Optional["torch.cuda.Stream"]:
+        """The call's stream, where ``call_ends`` has to mark it."""
+        home = self.home.cuda_stream
+        waits = attends and self.attended is not None and self.attended != handle
+        if handle == home and not waits:
+            if attends:
+                self.attended = handle
+            return None
+        stream = torch.cuda.ExternalStream(handle, device=self.device) if handle else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():   # its replays are the caller's to order
+                return None
+        if handle != home:
+            stream.wait_event(self.changed)
+        if waits:
+            if self.attended == home:
+                stream.wait_stream(self.home)
+            else:
+                stream.wait_event(self.calls[self.attended])
+        return stream
+
+    def call_ends(self, stream: "torch.cuda.Stream", attends: bool) -> None:
+        handle = stream.cuda_stream
+        if handle != self.home.cuda_stream:
+            self.calls.setdefault(handle, torch.cuda.Event()).record(stream)
+        if attends:
+            self.attended = handle
+
+
 class PagedCache:
     """A paged cache with its table and free pages, for a Cohort's requests.
 
     ``end[b]`` counts request b's tokens on the device, ``tokens[b]`` on the
     host, so that ``grow`` can hand out pages without waiting for the GPU.  The
-    table and ``end`` change on torch's current stream: the calls' stream is that
-    one or waits for it."""
+    table and ``end`` change on torch's current stream.  A call may go to any
+    stream: it comes after the changes made before it and before those made
+    after it, and one attention after the other (they share ``workspace``).
+    What calls on several streams write and read in the same pages is the
+    caller's to order, and so are a captured call's replays: behind the changes
+    that they need, never beside a change or another attention.  One host
+    thread uses a cache at a time."""
 
     def __init__(self, num_requests: int, num_q_heads: int, num_kv_heads: int, max_tokens: int, fmt: int = ss.SS_CACHE_MXFP8,
                  page_tokens: int = 64, num_pages: Optional[int] = None, max_rows: int = 1,
@@ -292,6 +353,7 @@ class PagedCache:
         self.tokens = [0] * num_requests
         self.owned: List[List[int]] = [[] for _ in range(num_requests)]
         self.free = list(range(pages))[::-1]
+        self.order = _Order(self.pages.device) if self.pages.is_cuda else None
 
     def _counts(self, rows: Sequence[int]) -> List[int]:
         rows = [operator.index(n) for n in rows]
@@ -305,12 +367,15 @@ class PagedCache:
         """``end`` and table entries change on torch's current stream.  The numbers travel in one copy from pinned
         memory, which torch hands out again only once that copy is done, so that the host waits for nothing."""
         x = torch.tensor(rows + places + ids, dtype=torch.int32)
-        if self.end.is_cuda:
+        if self.order is not None:
             x = x.pin_memory().to(self.end.device, non_blocking=True)
+            self.order.change_begins()
         n, m = len(rows), len(rows) + len(places)
         if ids:
             self.table.view(-1)[x[n:m]] = x[m:]
         self.end += x[:n]
+        if self.order is not None:
+            self.order.change_ends()
 
     def grow(self, rows: Sequence[int]) -> None:
         """Room for rows[b] more tokens of each request; ``end`` then counts them."""
@@ -349,6 +414,10 @@ class PagedCache:
         if torch.cuda.current_device() != device.index:
             raise ValueError(f"the cache is on {device}, the current device is {torch.cuda.current_device()}")
 
+    def _begins(self, stream: int, attends: bool) -> Optional["torch.cuda.Stream"]:
+        self._on_current_device()
+        return None if self.order is None else self.order.call_begins(stream, attends)
+
     def _counters(self, x: torch.Tensor, n: int, name: str) -> int:
         """Address of an int32 array of n, which the kernels read as it lies."""
         if not isinstance(x, torch.Tensor):
@@ -383,9 +452,11 @@ class PagedCache:
         if v.shape != k.shape or self._row_stride(v, self.desc.num_kv_heads) != stride:
             raise ValueError(f"k and v have one shape and one row stride (got {list(k.shape)} {k.stride()}, {list(v.shape)} {v.stride()})")
         starts = self._starts(row_start)
-        self._on_current_device()
+        on = self._begins(stream, False)
         ss.ss_cache_write(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), k.shape[0],
                           self.end.data_ptr(), starts, stride, stream)
+        if on is not None:
+            self.order.call_ends(on, False)
 
     def _chunk(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, kv_layout: int) -> None:
         """k and v hold num_rows tokens in the given layout: packed, or the views of one chunk of K and V rows."""
@@ -413,9 +484,11 @@ class PagedCache:
         num_rows tokens or more, or with SS_KV_HEAD_MAJOR_KV into one [heads, num_rows, 2, 128], v its second rows."""
         self._chunk(k, v, num_rows, kv_layout)
         ends, starts = self._counters(self.end if end is None else end, len(self.tokens), "end"), self._starts(row_start)
-        self._on_current_device()
+        on = self._begins(stream, False)
         ss.ss_cache_read(self.desc, self.pages.data_ptr(), self.table.data_ptr(), k.data_ptr(), v.data_ptr(), num_rows,
                          ends, starts, kv_layout, stream)
+        if on is not None:
+            self.order.call_ends(on, False)
 
     def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
                row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
@@ -426,9 +499,11 @@ class PagedCache:
                 raise ValueError(f"out, lse and prev are packed fp32 {list(q.shape)}, {list(q.shape[:2])} on {q.device} "
                                  f"(got {x.dtype} {list(x.shape)} on {x.device})")
         starts = self._starts(row_start)
-        self._on_current_device()
+        on = self._begins(stream, True)
         ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
                            self.end.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
                            starts, None if prev is None else prev[0].data_ptr(),
                            None if prev is None else prev[1].data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
                            stride, stream)
+        if on is not None:
+            self.order.call_ends(on, True)
