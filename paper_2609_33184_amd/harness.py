@@ -399,12 +399,14 @@ class PagedCache:
         rows = self._counts(rows)
         if any(n > t for n, t in zip(rows, self.tokens)):
             raise ValueError(f"a request holds fewer tokens than it is to release (holds {self.tokens}, releases {rows})")
+        places = []
         for b, n in enumerate(rows):
             self.tokens[b] -= n
-            keep = -(-self.tokens[b] // self.desc.page_tokens)
+            keep, at = -(-self.tokens[b] // self.desc.page_tokens), b * self.table.shape[1]
+            places += range(at + keep, at + len(self.owned[b]))
             self.free += self.owned[b][keep:]
             del self.owned[b][keep:]
-        self._post([-n for n in rows], [], [])
+        self._post([-n for n in rows], places, [-1] * len(places))
 
     def _on_current_device(self) -> None:
         """A call runs on the current device, wherever its addresses lead."""

@@ -159,3 +159,14 @@ def test_counts_are_whole_numbers():
         assert p.tokens == [33, 6] and p.end.tolist() == [33, 6] and all(type(n) is int for n in p.tokens)
         p.release(rows)
         assert p.tokens == [20, 5] and p.end.tolist() == [20, 5] and [len(x) for x in p.owned] == [2, 1]
+
+
+def test_released_pages_leave_the_table():
+    """What a request no longer owns it does not reach, whoever gets the page next."""
+    p = H.PagedCache(3, 8, 2, 100, ss.SS_CACHE_BF16, 16, num_pages=12, device="cpu")
+    p.grow([60, 17, 33])
+    for release, grow in (([30, 0, 1], [0, 40, 0]), ([0, 57, 0], [10, 0, 30]), ([40, 0, 62], [0, 0, 0])):
+        p.release(release)
+        p.grow(grow)
+        for b, owned in enumerate(p.owned):
+            assert p.table[b].tolist() == owned + [-1] * (p.table.shape[1] - len(owned))
