@@ -376,9 +376,10 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
 #define SS_CACHE_MXFP8 1
 #define SS_CACHE_MXFP4 2
 
-/* Most requests of one call, and KV heads of a cache. */
+/* Most requests of one call, KV heads of a cache, and rows of a write or read. */
 #define SS_CACHE_MAX_REQUESTS 4096
 #define SS_CACHE_MAX_KV_HEADS 512
+#define SS_CACHE_MAX_ROWS 268435440
 
 typedef struct {
   int32_t num_requests;     /* B, 1..SS_CACHE_MAX_REQUESTS                     */

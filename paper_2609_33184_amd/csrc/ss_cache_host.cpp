@@ -10,6 +10,9 @@
 
 namespace {
 
+// a workgroup of 256 threads takes 16 rows
+static_assert(((int64_t)SS_CACHE_MAX_ROWS + 15) / 16 * 256 < (int64_t(1) << 32), "a launch's threads are counted in 32 bits");
+
 using ss::fail;
 using ss::hip_fail;
 
@@ -61,7 +64,13 @@ ss_status check_attend_desc(const ss_cache_desc *d) {
   return SS_OK;
 }
 
-// The arguments that all calls share; *nothing: a call without rows.
+// What a write and a read share beside check_call's: a launch has fewer than 2^32 threads.
+ss_status check_rows(int32_t num_rows) {
+  if (num_rows > SS_CACHE_MAX_ROWS) return fail(SS_ERR_UNSUPPORTED, "num_rows %d > %d", num_rows, SS_CACHE_MAX_ROWS);
+  return SS_OK;
+}
+
+// The arguments that all calls share.
 ss_status check_call(const ss_cache_desc *d, const void *pages, const int32_t *page_table, int32_t num_rows,
                      const int32_t *row_start, const int32_t *end, hipStream_t stream) {
   if (pages == nullptr || !aligned(pages, 16)) return fail(SS_ERR_INVALID_ARGUMENT, "pages must be non-null and 16-byte aligned");
@@ -142,6 +151,8 @@ ss_status ss_cache_write(const ss_cache_desc *desc, void *pages, const int32_t *
   if (row_stride != 0 && (row_stride < packed || row_stride % 8 != 0))
     return fail(SS_ERR_INVALID_ARGUMENT, "row_stride must be 0 or a multiple of 8 of at least %lld elements (got %lld)",
                 (long long)packed, (long long)row_stride);
+  s = check_rows(num_rows);
+  if (s != SS_OK) return s;
   s = check_call(desc, pages, page_table, num_rows, row_start, end, stream);
   if (s != SS_OK) return s;
   ss::CacheRowsArgs p;
@@ -165,6 +176,8 @@ ss_status ss_cache_read(const ss_cache_desc *desc, const void *pages, const int3
     return fail(SS_ERR_INVALID_ARGUMENT, "kv_layout %d is none of the chunk layouts", kv_layout);
   if (kv_layout == SS_KV_HEAD_MAJOR_KV && static_cast<uint16_t *>(v) != static_cast<uint16_t *>(k) + ss::kCacheDim)
     return fail(SS_ERR_INVALID_ARGUMENT, "SS_KV_HEAD_MAJOR_KV takes v = k + head_dim elements");
+  s = check_rows(num_rows);
+  if (s != SS_OK) return s;
   s = check_call(desc, pages, page_table, num_rows, row_start, end, stream);
   if (s != SS_OK) return s;
   ss::CacheRowsArgs p;
