@@ -398,7 +398,8 @@ typedef struct {
                                SS_MAX_CANDIDATES, and max_rows * Hq / Hkv at
                                most SS_MAX_ROWS_PER_KV_HEAD; a request with
                                more rows counts there as one without rows      */
-  float softmax_scale;      /* sigma > 0, finite (attention only)              */
+  float softmax_scale;      /* sigma > 0, finite, times log2(e) too (attention
+                               only)                                           */
   int32_t causal;           /* attention: 1 = row i sees the tokens up to its
                                own position, 0 = all end[b]                    */
 } ss_cache_desc;

@@ -16,6 +16,8 @@ static_assert(((int64_t)SS_CACHE_MAX_ROWS + 15) / 16 * 256 < (int64_t(1) << 32),
 using ss::fail;
 using ss::hip_fail;
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 ss_status check_desc(const ss_cache_desc *d) {
@@ -58,8 +60,8 @@ ss_status check_attend_desc(const ss_cache_desc *d) {
   if ((int64_t)d->max_rows * (d->num_q_heads / d->num_kv_heads) > SS_MAX_ROWS_PER_KV_HEAD)
     return fail(SS_ERR_UNSUPPORTED, "rows per KV head %d x %d > %d", d->max_rows, d->num_q_heads / d->num_kv_heads,
                 SS_MAX_ROWS_PER_KV_HEAD);
-  if (!(d->softmax_scale > 0.f) || !std::isfinite(d->softmax_scale))
-    return fail(SS_ERR_INVALID_ARGUMENT, "softmax_scale must be positive and finite");
+  if (!(d->softmax_scale > 0.f) || !std::isfinite(d->softmax_scale * kLog2e))
+    return fail(SS_ERR_INVALID_ARGUMENT, "softmax_scale must be positive and finite, times log2(e) too (got %g)", (double)d->softmax_scale);
   if (d->causal != 0 && d->causal != 1) return fail(SS_ERR_INVALID_ARGUMENT, "causal must be 0 or 1 (got %d)", d->causal);
   return SS_OK;
 }
@@ -231,7 +233,7 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
   p.alone = layout.split.alone;
   p.piece_units = layout.split.piece_units;
   p.causal = desc->causal;
-  p.scale_log2 = desc->softmax_scale * 1.4426950408889634f;
+  p.scale_log2 = desc->softmax_scale * kLog2e;
   const hipError_t e = ss::launch_cache_attend(p, desc->format, stream);
   return e == hipSuccess ? SS_OK : hip_fail(e, "cache attention launch");
 }
