@@ -343,9 +343,12 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
  *                    and 4 scale bytes
  * A scale byte s stands for 2^(s - 127).  A block of 32 channels is written with
  * the smallest exponent e >= -111 for which no value exceeds F 2^e (F = 448 in
- * e4m3, 6 in e2m1) and each value x as x 2^-e rounded to nearest even.  A block
- * that holds a NaN or an infinity is written as scale byte 255 with codes 0, and
- * reads as 32 NaNs.  The bf16 format keeps every bit.
+ * e4m3, 6 in e2m1) and each value x as x 2^-e rounded to nearest even.  As in any
+ * rounding to nearest, the largest numbers may leave bf16's range: from 1.9375 x
+ * 2^127 (e4m3) or 1.75 x 2^127 (e2m1) on they become 2^128, which reads, and counts
+ * in the attention, as an infinity.  A block that holds a NaN or an infinity is
+ * written as scale byte 255 with codes 0, and reads as 32 NaNs.  The bf16 format
+ * keeps every bit.
  *
  * Conventions shared by the calls
  *   - Rows: request b has the rows row_start[b] .. row_start[b + 1] - 1 of k, v, q
@@ -429,7 +432,9 @@ size_t ss_cache_attend_workspace_bytes(const ss_cache_desc *desc);
  * over the tokens that the row sees.  q: device bf16, row r's head h at element
  * r * q_row_stride + h * d (0: packed, Hq * d).  out: device fp32 [num_rows, Hq,
  * d].  lse: null or device fp32 [num_rows, Hq], the natural-log sum of exp of the
- * scaled scores.  A row that sees nothing gets out 0 and lse -inf.
+ * scaled scores.  A row that sees nothing, or only scores of -inf, gets out 0 and
+ * lse -inf.  An infinity of V gives the rows that see it no finite number in its
+ * channel (an infinity or a NaN).
  * prev_out, prev_lse: both null, or an earlier part's out and lse over other
  * keys (a round's, or this call's over an earlier chunk of pages); the result is
  * then of both parts' keys together (Eq. 14).  A part whose lse is -inf does not

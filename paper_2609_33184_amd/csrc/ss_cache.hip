@@ -4,9 +4,10 @@
 //
 // Numbers.  A scaled block stands for code * 2^(byte - 127), code an OCP e4m3
 // or e2m1 number: v_cvt_scalef32 converts two of them with their scale in one
-// instruction, and every value of a finite block is a normal bf16 number, so
-// nothing is lost between the cache and the matrix instructions.  A scale byte
-// of 255 makes the conversion give NaN.
+// instruction, and every value of a finite block is zero or a normal bf16 number,
+// so nothing is lost between the cache and the matrix instructions (but 2^128, to
+// which the largest bf16 numbers round, is an infinity from there on).  A scale
+// byte of 255 makes the conversion give NaN.
 //
 // Rows.  Request b's row i of n_b stands for position end_b - n_b + i.  What a
 // table, an end or a row start could make unsafe is checked here: a page number
@@ -169,7 +170,8 @@ __device__ __forceinline__ void store_row(uint8_t *rows, uint8_t *scales, int sl
     int e = (int)((m + kCarry) >> 7) - kTop;
     e = e < 16 ? 16 : e;
     const float scale = scale_of((uint32_t)e);
-    // round to nearest even, exact otherwise: a power of two divides
+    // round to nearest even, exact otherwise: a power of two divides.  bf16's
+    // largest numbers round up to 2^128 (header)
     if constexpr (FMT == kCacheMx8) {
       u32x2_t code;
 #pragma unroll
