@@ -8,7 +8,7 @@ namespace ss {
 
 constexpr int kCacheDim = 128;          // channels of a row
 constexpr int kCacheTile = 32;          // tokens a wave attends per step
-constexpr int kCacheMaxRequests = 4096; // requests of one call: their starts and ends fit a workgroup's LDS
+constexpr int kCacheMaxRequests = 4096; // requests of one call: 64 chunks of 64, and their starts and ends fit a workgroup's LDS
 constexpr int kCacheBf16 = 0, kCacheMx8 = 1, kCacheMx4 = 2;
 
 // Bytes of one K or V row and of its scales, by format.

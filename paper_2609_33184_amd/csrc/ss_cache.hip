@@ -1043,7 +1043,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   const int b = blockIdx.x;
   const int item = blockIdx.y * kRowsPer + (tx >> 5) / SPLIT;     // of the request's heads and rows
   const int h = item / p.M, r = item - h * p.M;
-  // tiles of the requests before b, and of all, by every wave
+  // units (tiles and pieces' cost) of the requests before b, and of all, by every wave
   int before = 0, all = 0;
   for (int j = tx & 63; j < p.B; j += 64) {
     const int t = request_at(p, j).units;
@@ -1170,6 +1170,7 @@ CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M) {
   // wave: with 256 to 2048 pairs of 0 to 600 tokens in 8 bits 15.5, 16.3, 21.4 and
   // 27.0 us, workgroups 13.9, 17.3, 24.6 and 39.5; of 500 to 4000 tokens in 4 bits
   // with 24 rows 39.7, 52.6, 84.2 and 163, workgroups 34.7, 51.6, 86.3 and 165.
+  // More than 32 rows need two waves, so a worker there is always a workgroup.
   r.alone = M <= 32 && pairs >= 256 * kWaves;
   r.piece_units = r.alone ? kPieceAlone : kPieceGroup;
   const int64_t most = 256 * waves * (r.alone ? kWaves : 1);

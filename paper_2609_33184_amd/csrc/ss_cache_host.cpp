@@ -10,6 +10,8 @@
 
 namespace {
 
+// the attention counts the requests in chunks of 64, one lane for each of 64 chunks at most
+static_assert(SS_CACHE_MAX_REQUESTS <= ss::kCacheMaxRequests && ss::kCacheMaxRequests <= 64 * 64, "requests beyond a wave's chunks would be dropped");
 // a workgroup of 256 threads takes 16 rows
 static_assert(((int64_t)SS_CACHE_MAX_ROWS + 15) / 16 * 256 < (int64_t(1) << 32), "a launch's threads are counted in 32 bits");
 
