@@ -330,7 +330,7 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
  * written.  ss_cache_write appends rows, ss_cache_read takes rows out as a bf16
  * chunk (for ss_attend_history_chunk or a migration), ss_cache_attend attends
  * the pages where they lie: one token per request (plain decoding, drafting) or
- * a round's candidates.  A page is one contiguous range of bytes, so
+ * a round's candidates, not a prompt's own rows.  A page is one contiguous range of bytes, so
  * ss_download_range and ss_upload_chunk move whole pages between the tiers, in
  * 8 bits with half the link's bytes and in 4 bits with a quarter.
  *
