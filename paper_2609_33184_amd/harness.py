@@ -384,29 +384,33 @@ class PagedCache:
         more = [max(0, k - len(self.owned[b])) for b, k in enumerate(need)]
         if max(need) > self.table.shape[1] or sum(more) > len(self.free):
             raise MemoryError("the cache is full")
-        places, ids = [], []
+        places: List[int] = []
+        for b, k in enumerate(more):
+            at = b * self.table.shape[1] + len(self.owned[b])
+            places += range(at, at + k)
+        left = len(self.free) - len(places)
+        ids = self.free[left:][::-1]
+        self._post(rows, places, ids)
+        del self.free[left:]
+        new = iter(ids)
         for b, n in enumerate(rows):
             self.tokens[b] += n
-            at = b * self.table.shape[1] + len(self.owned[b])
-            new = [self.free.pop() for _ in range(more[b])]
-            self.owned[b] += new
-            places += range(at, at + len(new))
-            ids += new
-        self._post(rows, places, ids)
+            self.owned[b] += [next(new) for _ in range(more[b])]
 
     def release(self, rows: Sequence[int]) -> None:
         """The last rows[b] tokens of each request are rejected: their pages go back."""
         rows = self._counts(rows)
         if any(n > t for n, t in zip(rows, self.tokens)):
             raise ValueError(f"a request holds fewer tokens than it is to release (holds {self.tokens}, releases {rows})")
-        places = []
+        keep = [-(-(t - n) // self.desc.page_tokens) for n, t in zip(rows, self.tokens)]
+        places: List[int] = []
+        for b, k in enumerate(keep):
+            places += range(b * self.table.shape[1] + k, b * self.table.shape[1] + len(self.owned[b]))
+        self._post([-n for n in rows], places, [-1] * len(places))
         for b, n in enumerate(rows):
             self.tokens[b] -= n
-            keep, at = -(-self.tokens[b] // self.desc.page_tokens), b * self.table.shape[1]
-            places += range(at + keep, at + len(self.owned[b]))
-            self.free += self.owned[b][keep:]
-            del self.owned[b][keep:]
-        self._post([-n for n in rows], places, [-1] * len(places))
+            self.free += self.owned[b][keep[b]:]
+            del self.owned[b][keep[b]:]
 
     def _on_current_device(self) -> None:
         """A call runs on the current device, wherever its addresses lead."""

@@ -170,3 +170,23 @@ def test_released_pages_leave_the_table():
         p.grow(grow)
         for b, owned in enumerate(p.owned):
             assert p.table[b].tolist() == owned + [-1] * (p.table.shape[1] - len(owned))
+
+
+def test_a_change_that_fails_changes_nothing(monkeypatch):
+    """Memory that runs out, pinned or on the device, leaves the host's counts as they were."""
+    p = H.PagedCache(2, 8, 2, 64, ss.SS_CACHE_BF16, 16, device="cpu")
+    p.grow([20, 5])
+    state = lambda: (list(p.tokens), [list(x) for x in p.owned], list(p.free), p.table.tolist(), p.end.tolist())
+    before = state()
+
+    def full(*a, **kw):
+        raise RuntimeError("out of memory")
+
+    with monkeypatch.context() as m:
+        m.setattr(torch, "tensor", full)
+        for call, rows in ((p.grow, [30, 1]), (p.release, [20, 1])):
+            with pytest.raises(RuntimeError):
+                call(rows)
+            assert state() == before
+    p.grow([30, 1])
+    assert p.tokens == [50, 6] and p.table[0].tolist() == p.owned[0] and len(p.owned[0]) == 4
