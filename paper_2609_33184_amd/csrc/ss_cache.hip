@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
 //
 // What bounds it: bf16 is read at 6.7 TB/s (64 requests of 2048 to 65536 tokens,
 // 4.5 GB: 675 us, 664 with the arithmetic taken out); 8 and 4 bits with up to 16
-// rows at 6.1 and 5.2 (16 x 32768 tokens: 181 and 111 us); with 24 to 64 rows the
+// rows at 6.4 and 5.2 (16 x 32768 tokens: 174 and 110 us); with 24 to 64 rows the
 // vector and matrix instructions, which the SIMD issues one after the other (16 x
 // 32768 tokens in 4 bits with 24 rows: 155 to 185 us, 130 without its loads, 94
 // without its arithmetic); short requests the latency of a piece's first loads and
@@ -493,7 +493,8 @@ __device__ __forceinline__ void cut3(float p0, float p1, uint32_t &a, uint32_t &
 // Waves per SIMD that the registers are held to.  Up to 16 rows: 8 bits with one
 // and two 8 x 6000 tokens 29.1 and 24.7 us, 4 bits with two and three 16 x 32768
 // tokens 120 and 111; more rows: 8 and 4 bits with one and two 242 and 207, 209 and
-// 166 (24 rows).  bf16 with more rows does not fit two.
+// 166 (24 rows).  bf16 with more rows takes 312 registers and does not fit two: 16 x
+// 32768 tokens with 24 and 64 rows 338 and 498 us, 299 of them for the bytes.
 constexpr int attend_waves(int fmt, int nr) {
   if (nr == 32) return fmt == kCacheBf16 ? 1 : 2;
   return fmt == kCacheMx4 ? 3 : 2;
