@@ -373,7 +373,7 @@ def _own(state):
         if op == "window":
             ss.ss_cache_attend_window(desc, *cache, state["q"].data_ptr(), **to, **where)
         else:
-            ss.ss_cache_attend_tree(desc, *cache, q.data_ptr(), tree=state["tree"].data_ptr(), **to, **where)
+            ss.ss_cache_attend_tree(desc, *cache, state["q"].data_ptr(), tree=state["tree"].data_ptr(), **to, **where)
     if op == "keep":
         ss.ss_cache_keep(desc, *cache, kept=state["kept"].data_ptr(), num_kept=state["num_kept"].data_ptr(), **where)
 
