@@ -384,6 +384,11 @@ ss_status ss_download_range(void *dst_pinned_host, const void *src_device, size_
 #define SS_CACHE_MAX_KV_HEADS 512
 #define SS_CACHE_MAX_ROWS 268435440
 
+/* Most rows of a request's tree (bits of a row's word), and most of them times
+ * query heads on one KV head (at most SS_MAX_ROWS_PER_KV_HEAD of these). */
+#define SS_CACHE_MAX_TREE 64
+#define SS_CACHE_MAX_TREE_ROWS_PER_KV_HEAD 512
+
 typedef struct {
   int32_t num_requests;     /* B, 1..SS_CACHE_MAX_REQUESTS                     */
   int32_t num_q_heads;      /* Hq, a multiple of Hkv (attention only)          */
@@ -446,6 +451,86 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
                           int64_t q_row_stride, int32_t num_rows, const int32_t *row_start, const int32_t *end,
                           float *out, float *lse, const float *prev_out, const float *prev_lse, void *workspace,
                           size_t workspace_bytes, hipStream_t stream);
+
+/* Attend the cache with a sliding window: the row at position p sees the tokens t
+ * <= p with t > p - window (its own and the window - 1 before it) or t < sinks (the
+ * first tokens, which stay visible).  Everything else is as in ss_cache_attend,
+ * workspace and joining with an earlier part among it; desc->causal must be 1.
+ * window >= 1, sinks >= 0.  Only tiles of 32 tokens that some row may see are
+ * read, so pages that hold none of them may be given back (their table entries
+ * -1).  Values of any kind at tokens that a row does not see leave it as it is. */
+ss_status ss_cache_attend_window(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, int32_t window,
+                                 int32_t sinks, const void *q, int64_t q_row_stride, int32_t num_rows, const int32_t *row_start,
+                                 const int32_t *end, float *out, float *lse, const float *prev_out, const float *prev_lse,
+                                 void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ---- Trees of drafted tokens over the paged cache ---------------------------
+ * A request's last n_b tokens may be a tree instead of a chain of candidates: row i
+ * stands for its node i, whose K and V lie at position end[b] - n_b + i like any
+ * row's.  A step is ss_cache_append (the drafted rows enter, turned by their
+ * positions in the text, in which siblings are alike), ss_cache_attend_tree, and,
+ * once the target has chosen, ss_cache_keep, after which the accepted path is a
+ * chain behind the history and the caller's end[b] counts its tokens only. */
+
+/* How rows are turned by their positions: of each head the first rotary_dim
+ * channels, in pairs (j, j + rotary_dim / 2) or, interleaved, (2j, 2j + 1), pair j by
+ * the angle position * inv_freq[j]; y1 = scale (x1 cos - x2 sin), y2 = scale (x2 cos +
+ * x1 sin).  The other channels stay as they are, bit for bit. */
+typedef struct {
+  int32_t rotary_dim;       /* a multiple of 16, 16..128 (others up to 128: SS_ERR_UNSUPPORTED) */
+  int32_t interleaved;      /* 0 or 1                                          */
+  float scale;              /* > 0, finite; of sine and cosine, 1 as a rule    */
+  const float *inv_freq;    /* device [rotary_dim / 2], read when the call runs */
+} ss_rope_desc;
+
+/* Write rows into the cache, K turned: as ss_cache_write does with the turned rows
+ * rounded to bf16, bit for bit, in every format (a turned value is off by its
+ * rounding and 2^-22 of the pair's length at most).  positions: null (a row's
+ * position is its token's, end[b] - n_b + i) or device int32 [num_rows], of any
+ * sign (a history that lies elsewhere, a tree).  q, q_out: both null, or device
+ * bf16 rows r at element r * q_row_stride (q_out_row_stride; 0: packed, Hq * d) that
+ * are turned alike (num_q_heads matters then); q_out may be q with the same
+ * stride and must not overlap it otherwise, nor k and v.  A row whose token has no
+ * place is not written, but its q is turned; q_out's rows of no request stay as
+ * they were.  k, v, row_stride, num_rows: as in ss_cache_write. */
+ss_status ss_cache_append(const ss_cache_desc *desc, void *pages, const int32_t *page_table, const ss_rope_desc *rope,
+                          const int32_t *positions, const void *k, const void *v, int64_t row_stride, const void *q,
+                          int64_t q_row_stride, void *q_out, int64_t q_out_row_stride, int32_t num_rows,
+                          const int32_t *row_start, const int32_t *end, hipStream_t stream);
+
+/* Bytes of device workspace ss_cache_attend_tree needs with this descriptor, whatever
+ * the lengths; 0 if the descriptor is invalid (see ss_last_error). */
+size_t ss_cache_attend_tree_workspace_bytes(const ss_cache_desc *desc);
+
+/* Attend the cache with trees: row i of request b sees the tokens before position
+ * end[b] - n_b, and of the request's n_b last ones token j (position end[b] - n_b +
+ * j) where bit j of tree[row] is set, whatever its place: its own, as a rule, and
+ * its ancestors'.  Bits from n_b on do not count.  max_rows: at most
+ * SS_CACHE_MAX_TREE, times num_q_heads / num_kv_heads at most
+ * SS_CACHE_MAX_TREE_ROWS_PER_KV_HEAD; max_rows * num_q_heads at most 32768.  tree:
+ * device uint64 [num_rows], 8-byte aligned.  With window > 0 the row sees of the
+ * tokens before the tree only those t with t > p - window or t < sinks, p = end[b] -
+ * n_b + (set bits of its word) - 1: a row whose word holds its path stands as
+ * many places behind the history as it has ancestors.  window 0: no window.
+ * desc->causal does not matter.  Everything else is as in ss_cache_attend. */
+ss_status ss_cache_attend_tree(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const uint64_t *tree,
+                               int32_t window, int32_t sinks, const void *q, int64_t q_row_stride, int32_t num_rows,
+                               const int32_t *row_start, const int32_t *end, float *out, float *lse, const float *prev_out,
+                               const float *prev_lse, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Keep a path: of request b's last n_b tokens the kept ones move to the places from
+ * position end[b] - n_b on, K, V and scales bit for bit: token kept[r + j] (an index
+ * among the n_b, r the request's first row) to place j, for j < num_kept[b].  All
+ * are read before one is written, so they may come in any order, one several
+ * times.  An index outside [0, n_b), or one whose token has no place, leaves
+ * place j as it was, and so are the places from num_kept[b] on (a count outside 0
+ * .. n_b is taken as the nearer of the two).  kept: device int32 [num_rows];
+ * num_kept: device int32 [num_requests].  max_rows: at most SS_CACHE_MAX_TREE; a
+ * request with more rows stays as it is.  end: what the cache holds before the
+ * call, as in the attention. */
+ss_status ss_cache_keep(const ss_cache_desc *desc, void *pages, const int32_t *page_table, const int32_t *kept,
+                        const int32_t *num_kept, int32_t num_rows, const int32_t *row_start, const int32_t *end,
+                        hipStream_t stream);
 
 /* ---- I/O-aware dynamic verification width (paper Sec. 4.2) ----------------
  * Chooses the next round's width q (candidate rows per request, 1..8) as

@@ -20,6 +20,9 @@ Contents
     claims.
 ``cache``
     The paged cache: encode, decode, write, read and attend in float64.
+``tree``
+    Rows turned by their positions, attention over trees and windows of the
+    paged cache, and kept paths, in float64.
 ``bruteforce.verify_attention_decimal``
     The same definition written out element by element in 50-digit decimal
     arithmetic, for tiny inputs.

@@ -9,6 +9,7 @@ namespace ss {
 constexpr int kCacheDim = 128;          // channels of a row
 constexpr int kCacheTile = 32;          // tokens a wave attends per step
 constexpr int kCacheMaxRequests = 4096; // requests of one call: 64 chunks of 64, and their starts and ends fit a workgroup's LDS
+constexpr int kCacheMaxTree = 64;       // rows of a tree: bits of a row's word
 constexpr int kCacheBf16 = 0, kCacheMx8 = 1, kCacheMx4 = 2;
 
 // Bytes of one K or V row and of its scales, by format.
@@ -40,6 +41,23 @@ struct CacheRowsArgs : CacheArgs {
   int64_t head_stride;       // elements between a KV head and the next
 };
 
+struct CacheAppendArgs : CacheArgs {
+  const uint16_t *k, *v, *q;       // bf16 rows; q may be null
+  uint16_t *q_out;                 // may be q
+  int64_t row_stride, q_row_stride, q_out_row_stride;
+  const int32_t *positions;        // [num_rows], or null: the tokens' own
+  const float *inv_freq;           // [rotary_dim / 2]
+  float scale;                     // of sine and cosine
+  int32_t Hq;
+  int32_t rotary_dim;              // channels that turn, a multiple of 16
+  int32_t interleaved;             // pairs are neighbours, not half of rotary_dim apart
+};
+
+struct CacheKeepArgs : CacheArgs {
+  const int32_t *kept;             // [num_rows]: request b's from its first row's place on
+  const int32_t *num_kept;         // [B]
+};
+
 struct CacheAttendArgs : CacheArgs {
   const uint16_t *q;
   int64_t q_row_stride;
@@ -56,6 +74,17 @@ struct CacheAttendArgs : CacheArgs {
   float scale_log2;                     // softmax_scale * log2(e)
 };
 
+// Rows of one KV head that a piece of the attention below holds at most: more are
+// attended in blocks of as many.
+constexpr int kCacheRowBlock = 64;
+
+// Rows that see a tree, or a window and the first tokens, instead of a chain.
+struct CacheSeenArgs : CacheAttendArgs {
+  const uint64_t *tree;   // [num_rows]: bit j: the row sees the request's j-th row's token; null: a chain
+  int32_t window;         // tokens up to its own that a row sees of those before the request's rows; 0: all
+  int32_t sinks;          // first tokens that it sees as well
+};
+
 // How the attention over a cache of this kind is split; M query rows per KV head.
 struct CacheSplit {
   int workers;
@@ -63,10 +92,14 @@ struct CacheSplit {
   int piece_units;
 };
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
+inline int cache_row_blocks(int M) { return (M + kCacheRowBlock - 1) / kCacheRowBlock; }
 
 // Launch wrappers; return hipGetLastError() of the launch.
 hipError_t launch_cache_write(const CacheRowsArgs &p, int fmt, hipStream_t s);
 hipError_t launch_cache_read(const CacheRowsArgs &p, int fmt, hipStream_t s);
 hipError_t launch_cache_attend(const CacheAttendArgs &p, int fmt, hipStream_t s);
+hipError_t launch_cache_append(const CacheAppendArgs &p, int fmt, hipStream_t s);
+hipError_t launch_cache_keep(const CacheKeepArgs &p, int fmt, hipStream_t s);
+hipError_t launch_cache_attend_seen(const CacheSeenArgs &p, int fmt, hipStream_t s);
 
 }  // namespace ss

@@ -16,72 +16,12 @@
 #include <hip/hip_runtime.h>
 
 #include "ss_cache.h"
-
-#include <math.h>
+#include "ss_cache_device.h"
 
 #include <type_traits>
 
 namespace ss {
 namespace {
-
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x2_t __attribute__((ext_vector_type(2)));
-
-constexpr float kNegInf = -__builtin_huge_valf();
-constexpr int kBufferFlags = 0x00020000;   // buffer resource word 3: 32-bit data format, raw offsets
-constexpr int kStreamLoad = 2;             // non-temporal: the cache is read once per call
-constexpr int kThreads = 256;
-constexpr int kWaves = 4;
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Max / sum across the GROUPS (4 or 2) equal groups of lanes of a wave.
-template <int GROUPS>
-__device__ __forceinline__ float xgroup_max(float x) {
-  if constexpr (GROUPS == 4) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  }
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-template <int GROUPS>
-__device__ __forceinline__ float xgroup_sum(float x) {
-  if constexpr (GROUPS == 4) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  }
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-__device__ __forceinline__ s16x4_t lds_read_tr16(uint32_t at) {   // an LDS address
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(uintptr_t)at);
-}
-
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-// By value: __builtin_bit_cast of a vector's element takes its first one.
-__device__ __forceinline__ bf16x2_t as_bf16x2(uint32_t w) { return __builtin_bit_cast(bf16x2_t, w); }
-
-// The four (e4m3) or eight (e2m1) values of a dword, times scale, as bf16.
-__device__ __forceinline__ u32x2_t widen8(uint32_t w, float scale) {
-  return {__builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
-          __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
-}
-__device__ __forceinline__ u32x4_t widen4(uint32_t w, float scale) {
-  return {__builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
-          __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
-          __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
-          __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
-}
 
 // ---------------------------------------------------------------------------
 // Writing and reading rows.  A workgroup takes 16 rows and HEADS KV heads, 16
@@ -93,111 +33,6 @@ __device__ __forceinline__ u32x4_t widen4(uint32_t w, float scale) {
 // bits 43.5 us through the caches, 32 past them; 65536 tokens read from 8 bits 80
 // and 68, a copy's rate and a quarter more).
 // ---------------------------------------------------------------------------
-constexpr int kGroupRows = 16;
-
-// Where row t lives: its page block of KV head 0 and its slot there.
-struct Place {
-  uint8_t *page;   // null: nowhere
-  int slot;
-  bool row;        // whether t is a row of some request
-};
-
-// starts, ends: LDS, B + 1 and B words (none without row_start).
-__device__ __forceinline__ Place place_of(const CacheArgs &p, int64_t t, int tx, int32_t *starts, int32_t *ends) {
-  int b, e;
-  int64_t i, n;
-  if (p.row_start == nullptr) {
-    if (t >= p.num_rows) return {nullptr, 0, false};
-    b = (int)((uint32_t)t / (uint32_t)p.max_rows);
-    i = t - (int64_t)b * p.max_rows;
-    n = p.max_rows;
-    e = p.end[b];
-  } else {
-    for (int j = tx; j <= p.B; j += kThreads) {
-      starts[j] = p.row_start[j];
-      if (j < p.B) ends[j] = p.end[j];
-    }
-    __syncthreads();
-    // the last request that starts at or before t: an empty one's start is
-    // also the next one's, so it is never the last
-    int lo = 0, hi = p.B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (starts[mid] <= t)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    b = lo;
-    i = t - starts[b];
-    n = (int64_t)starts[b + 1] - starts[b];
-    if (t >= p.num_rows || i < 0 || i >= n) return {nullptr, 0, false};
-    e = ends[b];
-  }
-  const int64_t pos = e - n + i;
-  if (pos < 0 || pos >= p.capacity) return {nullptr, 0, true};
-  const int page = p.table[(int64_t)b * p.table_stride + (pos >> p.page_shift)];
-  if (page < 0 || page >= p.num_pages) return {nullptr, 0, true};
-  return {p.pages + (uint64_t)page * p.page_stride, (int)(pos & ((1 << p.page_shift) - 1)), true};
-}
-
-__device__ __forceinline__ uint32_t pack_max(uint32_t a, uint32_t b) {   // of two halves below 2^15 each
-  const uint32_t hi = (a & 0xffff0000u) > (b & 0xffff0000u) ? a & 0xffff0000u : b & 0xffff0000u;
-  const uint32_t lo = (a & 0xffffu) > (b & 0xffffu) ? a & 0xffffu : b & 0xffffu;
-  return hi | lo;
-}
-
-// Store a lane's 8 channels x (lane c of the row's 16) into row `slot` of the
-// rows at `rows` and the block's scale at `scales`.
-template <int FMT>
-__device__ __forceinline__ void store_row(uint8_t *rows, uint8_t *scales, int slot, int c, u32x4_t x) {
-  if constexpr (FMT == kCacheBf16) {
-    *reinterpret_cast<u32x4_t *>(rows + slot * 256 + 16 * c) = x;
-  } else {
-    // largest magnitude of the block, as bf16 bits, over the lane and its quad
-    uint32_t m = pack_max(pack_max(x[0] & 0x7fff7fffu, x[1] & 0x7fff7fffu), pack_max(x[2] & 0x7fff7fffu, x[3] & 0x7fff7fffu));
-    m = (m >> 16) > (m & 0xffffu) ? m >> 16 : m & 0xffffu;
-    uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xf, 0xf, false);   // quad_perm [1,0,3,2]
-    m = o > m ? o : m;
-    o = (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xf, 0xf, false);            // quad_perm [2,3,0,1]
-    m = o > m ? o : m;
-    // the smallest e with m <= F 2^e: F = 448 = 1.75 x 2^8 or 6 = 1.5 x 2^2.
-    // Adding what carries a fraction above F's into the exponent rounds up.
-    // Below 2^-111 a code's value would leave bf16's normal numbers.
-    constexpr uint32_t kCarry = FMT == kCacheMx8 ? 0x1f : 0x3f;
-    constexpr int kTop = FMT == kCacheMx8 ? 8 : 2;
-    const bool finite = m < 0x7f80u;
-    int e = (int)((m + kCarry) >> 7) - kTop;
-    e = e < 16 ? 16 : e;
-    const float scale = scale_of((uint32_t)e);
-    // round to nearest even, exact otherwise: a power of two divides.  bf16's
-    // largest numbers round up to 2^128 (header)
-    if constexpr (FMT == kCacheMx8) {
-      u32x2_t code;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        s16x2_t w = {0, 0};
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, as_bf16x2(x[2 * j]), scale, false);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, as_bf16x2(x[2 * j + 1]), scale, true);
-        code[j] = finite ? __builtin_bit_cast(uint32_t, w) : 0u;
-      }
-      *reinterpret_cast<u32x2_t *>(rows + slot * 128 + 8 * c) = code;
-    } else {
-      uint32_t code = 0;
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_bf16x2(x[0]), scale, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_bf16x2(x[1]), scale, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_bf16x2(x[2]), scale, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_bf16x2(x[3]), scale, 3);
-      *reinterpret_cast<uint32_t *>(rows + slot * 64 + 4 * c) = finite ? code : 0u;
-    }
-    // the row's four scale bytes as one word
-    uint32_t word = (finite ? (uint32_t)e : 255u) << (8 * (c >> 2));
-    word |= (uint32_t)__builtin_amdgcn_mov_dpp((int)word, 0x124, 0xf, 0xf, false);    // row_ror:4
-    word |= (uint32_t)__builtin_amdgcn_mov_dpp((int)word, 0x128, 0xf, 0xf, false);    // row_ror:8
-    if (c == 0) *reinterpret_cast<uint32_t *>(scales + 4 * slot) = word;
-  }
-}
-
 template <int FMT, int HEADS>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs p) {
   extern __shared__ int32_t starts[];
@@ -357,6 +192,40 @@ struct AttendLds {
   static constexpr int kBytes = kWaves * kVTile + kMerge;
 };
 
+// What the rows of a request see (SeenArgs).  With a window no row sees the tokens
+// between the sinks and the first row's window: of the request's tiles the first
+// `sinks` and those behind them and the gap are attended.
+template <typename Args>
+constexpr bool kSeen = std::is_same_v<Args, CacheSeenArgs>;
+struct Sight {
+  int sinks, gap;
+};
+template <typename Args>
+__device__ __forceinline__ Sight sight_of(const Args &p, int rows, int end, int len) {
+  Sight s = {0, 0};
+  if constexpr (kSeen<Args>) {
+    if (p.window > 0) {
+      const int all = (len + kCacheTile - 1) / kCacheTile;
+      const int64_t low = (int64_t)end - rows - p.window;      // below every row's window (a row of a tree that sees no node stands before it)
+      const int from = low <= 0 ? 0 : low >= len ? all : (int)low / kCacheTile;
+      s.sinks = ((p.sinks < len ? p.sinks : len) + kCacheTile - 1) / kCacheTile;
+      s.gap = from > s.sinks ? from - s.sinks : 0;
+    }
+  }
+  return s;
+}
+// Blocks that a request's rows of one KV head are attended in.
+template <typename Args>
+__device__ __forceinline__ int row_blocks(const Args &p, int rows) {
+  if constexpr (kSeen<Args>) return (rows * p.G + kCacheRowBlock - 1) / kCacheRowBlock;
+  return 1;
+}
+// Rows of a piece's state.
+template <typename Args>
+__device__ __forceinline__ int part_rows(const Args &p) {
+  return kSeen<Args> && p.M > kCacheRowBlock ? kCacheRowBlock : p.M;
+}
+
 // A request as the attention needs it; in a window, lane i holds request base + i.
 struct Request {
   int rows;      // n_b: 0 if there are more than max_rows or fewer than none
@@ -366,7 +235,8 @@ struct Request {
   int tiles;
   int units;     // what the shares count: the tiles and the cost of a piece
 };
-__device__ __forceinline__ Request request_at(const CacheAttendArgs &p, int b) {
+template <typename Args>
+__device__ __forceinline__ Request request_at(const Args &p, int b) {
   Request r;
   const int c = b < p.B ? b : p.B - 1;     // loads without a branch, so that several calls' overlap
   r.end = p.end[c];
@@ -381,8 +251,53 @@ __device__ __forceinline__ Request request_at(const CacheAttendArgs &p, int b) {
   r.rows = b < p.B ? r.rows : 0;
   r.len = r.end < 0 ? 0 : r.end > p.capacity ? p.capacity : r.end;
   r.tiles = r.rows == 0 ? 0 : (r.len + kCacheTile - 1) / kCacheTile;
-  r.units = r.tiles == 0 ? 0 : r.tiles + p.piece_units;
+  if constexpr (kSeen<Args>) r.tiles = r.rows == 0 ? 0 : r.tiles - sight_of(p, r.rows, r.end, r.len).gap;
+  r.units = r.tiles == 0 ? 0 : row_blocks(p, r.rows) * (r.tiles + p.piece_units);
   return r;
+}
+
+// Which tokens a row sees: those before the request's rows, from `low` on or below
+// `sinks`, and of its n last tokens, from `first` on, those whose bit is set.
+struct Seen {
+  uint64_t bits;
+  int64_t first;      // position of the request's first row
+  int low, sinks;     // no window: 0, 0
+  int len;
+  int all_from, all_to;     // between these every row sees every token
+  __device__ __forceinline__ bool whole(int tok) const {
+    return tok + kCacheTile <= all_to && (tok >= all_from || tok + kCacheTile <= sinks);
+  }
+  static __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+  __device__ __forceinline__ uint32_t word(int tok) const {
+    const int64_t far = tok - first;
+    const int rel = far > 64 ? 64 : far < -32 ? -32 : (int)far;
+    const uint32_t before = below(-rel) & (~below(low - tok) | below(sinks - tok));
+    const uint32_t tree = rel >= 64 ? 0u : rel >= 0 ? (uint32_t)(bits >> rel) : (uint32_t)(bits << -rel);
+    return (before | tree) & below(len - tok);
+  }
+};
+// Of row i of a request's n, the row0 + i-th of the call.
+__device__ __forceinline__ Seen seen_by(const CacheSeenArgs &p, int n, int row0, int end, int len, int i) {
+  const int64_t row = (int64_t)row0 + i;
+  Seen s;
+  s.first = (int64_t)end - n;
+  s.len = len;
+  s.sinks = p.sinks;
+  uint64_t bits = i < n && row >= 0 && row < p.num_rows ? p.tree != nullptr ? p.tree[row] : (2ull << i) - 1 : 0;
+  bits &= n >= 64 ? ~0ull : (1ull << n) - 1;
+  const auto clamp = [](int64_t x) { return x < 0 ? 0 : x > 0x7fffffff ? 0x7fffffff : (int)x; };
+  const int64_t low = s.first + __popcll(bits) - p.window;      // the row's position is first + its nodes - 1
+  s.low = p.window > 0 ? clamp(low) : 0;
+  if (p.tree == nullptr && p.window > 0) {      // a chain's window may reach into it; a tree's word says all
+    const int hides = clamp(s.low - s.first), sink = clamp(s.sinks - s.first);
+    const uint64_t sinks = sink >= 64 ? ~0ull : (1ull << sink) - 1;
+    bits &= (hides >= 64 ? 0ull : ~0ull << hides) | sinks;
+  }
+  s.bits = bits;
+  const int to = clamp(s.first);
+  s.all_to = to < len ? to : len;
+  s.all_from = p.window > 0 ? clamp(s.first + n - p.window) : 0;
+  return s;
 }
 
 // x as a value that the compiler has not seen: of the thread's index, so that it
@@ -500,8 +415,8 @@ constexpr int attend_waves(int fmt, int nr) {
   return fmt == kCacheMx4 ? 3 : 2;
 }
 
-template <int FMT, int NR, int HALVES, int STREAMS>
-__global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_kernel(CacheAttendArgs p) {
+template <int FMT, int NR, int HALVES, int STREAMS, typename Args>
+__global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_kernel(Args p) {
   using Lds = AttendLds<NR, STREAMS>;
   static_assert(STREAMS * HALVES == kWaves || (STREAMS == 1 && HALVES == 1), "a workgroup's waves, or each for itself");
   using Acc = typename Mfma<NR>::Acc;
@@ -575,24 +490,32 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     int h, t0, tiles;
     int count;     // this wave's tiles: t0 + ws, + STREAMS, ...
     int ids;       // lane j: page of half tile j of them, -1 for what is none
+    int block;     // of its rows (SeenArgs)
+    Sight sight;
+  };
+  // The request's tile that is the t-th attended one.
+  auto tile_at = [&](const Piece &q, int t) {
+    if constexpr (kSeen<Args>) return t < q.sight.sinks ? t : t + q.sight.gap;
+    return t;
   };
   // Pages of the wave's tiles k0 .. k0 + 31 of a piece.
   auto pages_of = [&](const Piece &q, int k0) {
     const int lane = hidden(thread & 63);
     const int k = k0 + (lane >> 1);
-    const int64_t tok = (int64_t)(q.t0 + ws + STREAMS * k) * kCacheTile + 16 * (lane & 1);
+    const int64_t tok = (int64_t)tile_at(q, q.t0 + ws + STREAMS * k) * kCacheTile + 16 * (lane & 1);
     int id = -1;
     if (k < q.count && tok < q.len) id = p.table[(int64_t)q.b * p.table_stride + (tok >> p.page_shift)];
     return id >= 0 && id < p.num_pages ? id : -1;
   };
   auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   auto uniform = [&](const Piece &q) {     // the wave's, in scalar registers
-    return Piece{one(q.b), one(q.rows), one(q.row0), one(q.end), one(q.len), one(q.whole), one(q.h), one(q.t0), one(q.tiles), one(q.count), q.ids};
+    return Piece{one(q.b), one(q.rows), one(q.row0), one(q.end), one(q.len), one(q.whole), one(q.h), one(q.t0), one(q.tiles), one(q.count), q.ids, one(q.block),
+                 {one(q.sight.sinks), one(q.sight.gap)}};
   };
   // The share's next piece.  Its units are the piece's cost, then the tiles: a
   // share that ends within the cost leaves the tiles to the next one.
   auto next_piece = [&]() {
-    Piece q = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1};
+    Piece q = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1, 0, {0, 0}};
     while (left > 0) {
       const uint64_t more = idx < 64 ? __builtin_amdgcn_ballot_w64(win.units > 0) & (~0ull << idx) : 0;
       if (more == 0) {
@@ -607,10 +530,23 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
       }
       idx = __builtin_ctzll(more);
       const int units = lane_of(win.units, idx), cost = p.piece_units;
-      const int take = units - skip < left ? units - skip : left;
-      const int t0 = skip > cost ? skip - cost : 0, t1 = skip + take > cost ? skip + take - cost : 0;
+      int take, t0, t1;
+      bool ends = true;          // whether the request's units do
+      if constexpr (kSeen<Args>) {
+        const int per = lane_of(win.tiles, idx) + cost;
+        q.block = units > per ? skip / per : 0;
+        const int off = skip - q.block * per;
+        take = per - off < left ? per - off : left;
+        t0 = off > cost ? off - cost : 0, t1 = off + take > cost ? off + take - cost : 0;
+        skip += take;
+        ends = skip >= units;
+        if (ends) skip = 0;
+      } else {
+        take = units - skip < left ? units - skip : left;
+        t0 = skip > cost ? skip - cost : 0, t1 = skip + take > cost ? skip + take - cost : 0;
+        skip = 0;
+      }
       left -= take;
-      skip = 0;
       if (t1 > t0) {
         q.b = base + idx;
         q.rows = lane_of(win.rows, idx);
@@ -622,11 +558,12 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
         q.t0 = t0;
         q.tiles = t1 - t0;
         q.count = q.tiles <= ws ? 0 : (q.tiles - ws + STREAMS - 1) / STREAMS;
+        q.sight = sight_of(p, q.rows, q.end, q.len);
         q.ids = pages_of(q, 0);
-        ++idx;
+        if (ends) ++idx;
         break;
       }
-      ++idx;
+      if (ends) ++idx;
     }
     left = one(left);
     idx = one(idx);
@@ -707,7 +644,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   // Queries of a piece: B operand of k-step s, row lr, the chunk of 8 channels that K's lanes hold there
   bf16x8_t qop[kSteps];
   auto load_q = [&](const Piece &q) {
-    const int lane = hidden(thread & 63), r = NR * half + lane % NR, lq = lane / NR;
+    const int lane = hidden(thread & 63), r = kCacheRowBlock * q.block + NR * half + lane % NR, lq = lane / NR;
     const int i = (int)((uint32_t)r * p.g_inv >> 16);      // r / G
     const int64_t row = (int64_t)q.row0 + i;
     const bool ok = r < q.rows * p.G && row >= 0 && row < p.num_rows;
@@ -779,7 +716,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     const bool here = k < cp.count;
     if (!here && np.tiles == 0) return;
     asm volatile("" : "+s"(k));      // or the loop keeps copies of what depends on it, 40 registers of them
-    const Where at = find((here ? cp.t0 + ws + STREAMS * k : np.t0 + ws) * kCacheTile, here ? cp.len : np.len, here ? cp.h : np.h,
+    const Where at = find((here ? tile_at(cp, cp.t0 + ws + STREAMS * k) : tile_at(np, np.t0 + ws)) * kCacheTile, here ? cp.len : np.len, here ? cp.h : np.h,
                           here ? ids : np.ids, here ? 2 * (k & 31) : 0);
     if (!here) load_q(np);
     load_k(at);
@@ -788,7 +725,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   };
   float x[kScores];
   {
-    const Where at = find((cp.t0 + ws) * kCacheTile, cp.len, cp.h, cp.ids, 0);
+    const Where at = find(tile_at(cp, cp.t0 + ws) * kCacheTile, cp.len, cp.h, cp.ids, 0);
     load_q(cp);
     load_k(at);
     load_v(at);
@@ -797,13 +734,16 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   }
 
   while (true) {
-    const int n = cp.rows, M = n * p.G, len = cp.len, row0 = cp.row0, end = cp.end, h = cp.h, t0 = cp.t0;
+    const int n = cp.rows, first_row = kCacheRowBlock * cp.block, M = kSeen<Args> && n * p.G - first_row > kCacheRowBlock ? kCacheRowBlock : n * p.G - first_row;
+    const int len = cp.len, row0 = cp.row0, end = cp.end, h = cp.h, t0 = cp.t0;
     int tx = hidden(thread);
     const int lane = tx & 63, lr = lane % NR;
     uint32_t hole = gone;      // of the tile that x belongs to
     ids_next = pages_of(cp, 32);
     load_tile(1);
 
+    Seen seen;
+    if constexpr (kSeen<Args>) seen = seen_by(p, n, row0, end, len, (int)((uint32_t)(first_row + NR * half + lr) * p.g_inv >> 16));
     // tokens that the lane's row sees, and that every row sees
     const int64_t last = (int64_t)end - n + 1 + (int)((uint32_t)(NR * half + lr) * p.g_inv >> 16);
     const int limit = p.causal && last < len ? (last < 0 ? 0 : (int)last) : len;
@@ -819,9 +759,19 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     do {
       const int lane = hidden(tx & 63);
       const int lr = lane % NR, lq = lane / NR;
-      const int tok = (t0 + ws + STREAMS * k) * kCacheTile;
-      const bool mixed = p.causal && tok + kCacheTile > all_see;
-      if (hole != 0 || tok + kCacheTile > all_see) {
+      const int tok = tile_at(cp, t0 + ws + STREAMS * k) * kCacheTile;
+      const bool mixed = kSeen<Args> ? !seen.whole(tok) : p.causal && tok + kCacheTile > all_see;
+      uint32_t word = 0;         // tokens of the tile that the lane's row sees
+      if constexpr (kSeen<Args>) {
+        if (hole != 0 || mixed) {
+          word = seen.word(tok) & ((hole & 1u ? 0u : 0xffffu) | (hole & 2u ? 0u : 0xffff0000u));
+#pragma unroll
+          for (int e = 0; e < kScores; ++e) {
+            const int t = 4 * kGroups * (e >> 2) + 4 * lq + (e & 3);
+            x[e] = (word >> t) & 1u ? x[e] : kNegInf;
+          }
+        }
+      } else if (hole != 0 || tok + kCacheTile > all_see) {
 #pragma unroll
         for (int e = 0; e < kScores; ++e) {
           const int t = 4 * kGroups * (e >> 2) + 4 * lq + (e & 3);
@@ -844,7 +794,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
       if (mixed) {
         // Values that are no numbers at tokens that some rows see and others do
         // not: a weight of zero would spread them.  Such tokens, SS_MAX_CANDIDATES -
-        // 1 at most, are then added one by one to the rows that see them, and
+        // 1 at most (all of a tile that a window or a tree cuts), are then added one by one to the rows that see them, and
         // their V rows are cleared for the others.
         bool odd = false;
 #pragma unroll
@@ -854,7 +804,8 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
           for (int e = 0; e < 4; ++e) odd |= (y[e] & 0x7f80u) == 0x7f80u || (y[e] & 0x7f800000u) == 0x7f800000u;
         }
         const int stop = __builtin_amdgcn_ballot_w64(odd) == 0 ? 0 : len - tok < kCacheTile ? len - tok : kCacheTile;
-        for (int t = all_see > tok ? all_see - tok : 0; t < stop; ++t) {
+        for (int t = !kSeen<Args> && all_see > tok ? all_see - tok : 0; t < stop; ++t) {
+          if (kSeen<Args> && __builtin_amdgcn_ballot_w64((word >> t) & 1u) == ~0ull) continue;
           unsigned char *row = vs_lds + t * kLdsRow;
           const int e = 4 * (t / (4 * kGroups)) + (t & 3);
           float xe = 0.f;
@@ -862,7 +813,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
           for (int j = 0; j < kScores; ++j) xe = j == e ? x[j] : xe;
           xe = __shfl(xe, lr + NR * ((t >> 2) % kGroups));
           const float pe = exp2_fast(__builtin_fmaf(xe, p.scale_log2, -ms));
-          if (tok + t < limit) {
+          if (kSeen<Args> ? (word >> t) & 1u : tok + t < limit) {
 #pragma unroll
             for (int c = 0; c < kChans; ++c) {
               const int at = 4 * kGroups * c + 4 * lq;     // the piece's first channel
@@ -937,8 +888,8 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     auto finish = [&](int r, int seg, auto segs, float m, float l, auto piece_at) {
       constexpr int kSegs = decltype(segs)::value, kPieces = kCacheDim / 4 / kSegs;
       if (cp.tiles == cp.whole) {
-        const int i = (int)((uint32_t)r * p.g_inv >> 16);
-        const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + r - i * p.G;
+        const int rb = first_row + r, i = (int)((uint32_t)rb * p.g_inv >> 16);
+        const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + rb - i * p.G;
         if (row0 + i >= 0 && row0 + i < p.num_rows) {
           const RowEnd end = row_end(p, row, m, l);
 #pragma unroll
@@ -950,7 +901,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
         }
       } else {
         // two states per worker at most: of a pair that starts before the share, and of one that ends behind it
-        const int64_t o = (int64_t)(2 * worker + (t0 == 0 ? 1 : 0)) * p.M + r;
+        const int64_t o = (int64_t)(2 * worker + (t0 == 0 ? 1 : 0)) * part_rows(p) + r;
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) *reinterpret_cast<f32x4_t *>(p.part_a + o * kCacheDim + 4 * (seg + kSegs * k)) = piece_at(k);
         if (seg == 0) *reinterpret_cast<f32x2_t *>(p.part_ml + 2 * o) = f32x2_t{m, l};
@@ -1036,8 +987,8 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
 // 8 where a pair may have that many: 32768 tokens with 4 heads, 128 states a pair,
 // 8.8 us with 8 and 6.3 with 32), else each takes a row of its own.
 // ---------------------------------------------------------------------------
-template <int SPLIT>
-__global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_kernel(CacheAttendArgs p) {
+template <int SPLIT, typename Args>
+__global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_kernel(Args p) {
   constexpr int kHalves = SPLIT > 8 ? SPLIT : 8, kRowsPer = kHalves / SPLIT;
   const int tx = threadIdx.x, lane = tx & 31;
   const int part = (tx >> 5) % SPLIT;
@@ -1061,8 +1012,9 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   f32x4_t a = {0.f, 0.f, 0.f, 0.f};
   if (q.tiles > 0) {
     const int share = share_of(all * p.Hkv, p.workers);
-    const int start = h * all + before;
-    const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + q.units - 1) / (uint32_t)share);
+    const int block = kSeen<Args> ? r / kCacheRowBlock : 0, units = q.tiles + p.piece_units;
+    const int start = h * all + before + block * units;
+    const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + units - 1) / (uint32_t)share);
     mine &= w0 != w1;               // else one worker attended all of it
     if (mine) {
       constexpr int kAhead = SPLIT > 8 ? 4 : 8;     // states in flight
@@ -1072,7 +1024,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
           const int v = w + j * SPLIT <= w1 ? w + j * SPLIT : w1;
-          const int64_t o = (int64_t)(2 * v + (v == w0 ? 1 : 0)) * p.M + r;
+          const int64_t o = (int64_t)(2 * v + (v == w0 ? 1 : 0)) * part_rows(p) + r - block * kCacheRowBlock;
           ml[j] = *reinterpret_cast<const f32x2_t *>(p.part_ml + 2 * o);
           x[j] = *reinterpret_cast<const f32x4_t *>(p.part_a + o * kCacheDim + 4 * lane);
         }
@@ -1134,30 +1086,30 @@ hipError_t launch_rows(const CacheRowsArgs &p, F1 one, F4 four, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int FMT>
-hipError_t attend(const CacheAttendArgs &p, hipStream_t s) {
+template <int FMT, typename Args>
+hipError_t attend(const Args &p, hipStream_t s) {
   if (p.alone) {
     const dim3 grid((p.workers + kWaves - 1) / kWaves);
     if (p.M <= 16)
-      hipLaunchKernelGGL((cache_attend_kernel<FMT, 16, 1, 1>), grid, dim3(kThreads), 0, s, p);
+      hipLaunchKernelGGL((cache_attend_kernel<FMT, 16, 1, 1, Args>), grid, dim3(kThreads), 0, s, p);
     else
-      hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 1, 1>), grid, dim3(kThreads), 0, s, p);
+      hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 1, 1, Args>), grid, dim3(kThreads), 0, s, p);
   } else if (p.M <= 16) {
-    hipLaunchKernelGGL((cache_attend_kernel<FMT, 16, 1, 4>), dim3(p.workers), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_attend_kernel<FMT, 16, 1, 4, Args>), dim3(p.workers), dim3(kThreads), 0, s, p);
   } else if (p.M <= 32) {
-    hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 1, 4>), dim3(p.workers), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 1, 4, Args>), dim3(p.workers), dim3(kThreads), 0, s, p);
   } else {
-    hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 2, 2>), dim3(p.workers), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_attend_kernel<FMT, 32, 2, 2, Args>), dim3(p.workers), dim3(kThreads), 0, s, p);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t pairs = (int64_t)p.B * p.Hkv;
+  const int64_t pairs = (int64_t)p.B * p.Hkv * cache_row_blocks(p.M);
   if (pairs * 32 <= p.workers)
-    hipLaunchKernelGGL((cache_join_kernel<32>), dim3(p.B, p.Hkv * p.M), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL((cache_join_kernel<32, Args>), dim3(p.B, p.Hkv * p.M), dim3(1024), 0, s, p);
   else if (pairs * 8 <= p.workers)
-    hipLaunchKernelGGL((cache_join_kernel<8>), dim3(p.B, p.Hkv * p.M), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_join_kernel<8, Args>), dim3(p.B, p.Hkv * p.M), dim3(kThreads), 0, s, p);
   else
-    hipLaunchKernelGGL((cache_join_kernel<1>), dim3(p.B, (p.Hkv * p.M + 7) / 8), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((cache_join_kernel<1, Args>), dim3(p.B, (p.Hkv * p.M + 7) / 8), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -1175,7 +1127,7 @@ CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M) {
   r.alone = M <= 32 && pairs >= 256 * kWaves;
   r.piece_units = r.alone ? kPieceAlone : kPieceGroup;
   const int64_t most = 256 * waves * (r.alone ? kWaves : 1);
-  const int64_t units = pairs * ((capacity + kCacheTile - 1) / kCacheTile + r.piece_units);
+  const int64_t units = pairs * cache_row_blocks(M) * ((capacity + kCacheTile - 1) / kCacheTile + r.piece_units);
   const int64_t need = (units + kMinShare - 1) / kMinShare;
   r.workers = (int)(need < most ? need : most);
   return r;
@@ -1193,10 +1145,13 @@ hipError_t launch_cache_read(const CacheRowsArgs &p, int fmt, hipStream_t s) {
   return launch_rows<kCacheMx4>(p, cache_read_kernel<kCacheMx4, 1>, cache_read_kernel<kCacheMx4, 4>, s);
 }
 
-hipError_t launch_cache_attend(const CacheAttendArgs &p, int fmt, hipStream_t s) {
+template <typename Args>
+static hipError_t attend_of(const Args &p, int fmt, hipStream_t s) {
   if (fmt == kCacheBf16) return attend<kCacheBf16>(p, s);
   if (fmt == kCacheMx8) return attend<kCacheMx8>(p, s);
   return attend<kCacheMx4>(p, s);
 }
+hipError_t launch_cache_attend(const CacheAttendArgs &p, int fmt, hipStream_t s) { return attend_of(p, fmt, s); }
+hipError_t launch_cache_attend_seen(const CacheSeenArgs &p, int fmt, hipStream_t s) { return attend_of(p, fmt, s); }
 
 }  // namespace ss

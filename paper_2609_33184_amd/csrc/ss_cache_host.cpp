@@ -13,6 +13,10 @@ namespace {
 // the attention counts the requests in chunks of 64, one lane for each of 64 chunks at most
 static_assert(SS_CACHE_MAX_REQUESTS <= ss::kCacheMaxRequests && ss::kCacheMaxRequests <= 64 * 64, "requests beyond a wave's chunks would be dropped");
 // a workgroup of 256 threads takes 16 rows
+// a row's word has a bit for every node; keeping a path holds a tree's rows in registers
+static_assert(SS_CACHE_MAX_TREE == ss::kCacheMaxTree && SS_CACHE_MAX_TREE == 64, "nodes of a tree are bits of 64");
+// rows of a KV head are divided by G with a multiplication, exact where row x G < 2^16
+static_assert(SS_CACHE_MAX_TREE_ROWS_PER_KV_HEAD * SS_MAX_ROWS_PER_KV_HEAD < 65536, "a row's query and head come from a multiplication");
 static_assert(((int64_t)SS_CACHE_MAX_ROWS + 15) / 16 * 256 < (int64_t(1) << 32), "a launch's threads are counted in 32 bits");
 
 using ss::fail;
@@ -51,20 +55,42 @@ ss_status check_desc(const ss_cache_desc *d) {
   return SS_OK;
 }
 
-ss_status check_attend_desc(const ss_cache_desc *d) {
+// most, most_per_head: rows of a request, and of them and the query heads on one KV head
+ss_status check_attend_desc(const ss_cache_desc *d, int most = SS_MAX_CANDIDATES, int most_per_head = SS_MAX_ROWS_PER_KV_HEAD) {
   const ss_status s = check_desc(d);
   if (s != SS_OK) return s;
   if (d->num_q_heads < 1 || d->num_q_heads % d->num_kv_heads != 0)
     return fail(SS_ERR_INVALID_ARGUMENT, "num_q_heads must be a positive multiple of num_kv_heads (got %d, %d)",
                 d->num_q_heads, d->num_kv_heads);
-  if (d->max_rows > SS_MAX_CANDIDATES)
-    return fail(SS_ERR_INVALID_ARGUMENT, "max_rows must be at most %d for an attention (got %d)", SS_MAX_CANDIDATES, d->max_rows);
-  if ((int64_t)d->max_rows * (d->num_q_heads / d->num_kv_heads) > SS_MAX_ROWS_PER_KV_HEAD)
-    return fail(SS_ERR_UNSUPPORTED, "rows per KV head %d x %d > %d", d->max_rows, d->num_q_heads / d->num_kv_heads,
-                SS_MAX_ROWS_PER_KV_HEAD);
+  if (d->max_rows > most)
+    return fail(SS_ERR_INVALID_ARGUMENT, "max_rows must be at most %d for an attention (got %d)", most, d->max_rows);
+  if ((int64_t)d->max_rows * (d->num_q_heads / d->num_kv_heads) > most_per_head)
+    return fail(SS_ERR_UNSUPPORTED, "rows per KV head %d x %d > %d", d->max_rows, d->num_q_heads / d->num_kv_heads, most_per_head);
   if (!(d->softmax_scale > 0.f) || !std::isfinite(d->softmax_scale * kLog2e))
     return fail(SS_ERR_INVALID_ARGUMENT, "softmax_scale must be positive and finite, times log2(e) too (got %g)", (double)d->softmax_scale);
   if (d->causal != 0 && d->causal != 1) return fail(SS_ERR_INVALID_ARGUMENT, "causal must be 0 or 1 (got %d)", d->causal);
+  return SS_OK;
+}
+
+ss_status check_tree_desc(const ss_cache_desc *d) {
+  const ss_status s = check_attend_desc(d, SS_CACHE_MAX_TREE, SS_CACHE_MAX_TREE_ROWS_PER_KV_HEAD);
+  if (s != SS_OK) return s;
+  if (d->num_q_heads / d->num_kv_heads > SS_MAX_ROWS_PER_KV_HEAD)
+    return fail(SS_ERR_UNSUPPORTED, "query heads per KV head %d > %d", d->num_q_heads / d->num_kv_heads, SS_MAX_ROWS_PER_KV_HEAD);
+  // a launch's grid has a workgroup for every row and head of a request, at most
+  if ((int64_t)d->max_rows * d->num_q_heads > 32768)
+    return fail(SS_ERR_UNSUPPORTED, "max_rows x num_q_heads %d x %d > 32768", d->max_rows, d->num_q_heads);
+  // tiles of all requests, heads and blocks of rows are counted in 32 bits
+  const int64_t tiles = ((int64_t)d->table_stride * d->page_tokens + ss::kCacheTile - 1) / ss::kCacheTile * d->num_requests;
+  const int blocks = ss::cache_row_blocks(d->max_rows * (d->num_q_heads / d->num_kv_heads));
+  if (tiles > (int64_t(1) << 30) / d->num_kv_heads / blocks)
+    return fail(SS_ERR_UNSUPPORTED, "num_requests x table_stride x num_kv_heads x %d blocks of rows reaches more than 2^35 tokens", blocks);
+  return SS_OK;
+}
+
+ss_status check_window(int32_t window, int32_t sinks, int32_t least) {
+  if (window < least || sinks < 0)
+    return fail(SS_ERR_INVALID_ARGUMENT, "window must be >= %d and sinks >= 0 (got %d, %d)", least, window, sinks);
   return SS_OK;
 }
 
@@ -124,11 +150,52 @@ struct AttendLayout {
   explicit AttendLayout(const ss_cache_desc *d) {
     M = d->max_rows * (d->num_q_heads / d->num_kv_heads);
     split = ss::cache_attend_split(d->format, d->num_requests, d->num_kv_heads, d->table_stride * d->page_tokens, M);
-    const size_t rows = 2 * (size_t)split.workers * (size_t)M;
+    const size_t rows = 2 * (size_t)split.workers * (size_t)(M < ss::kCacheRowBlock ? M : ss::kCacheRowBlock);
     ml = rows * ss::kCacheDim * sizeof(float);
     bytes = (ml + rows * 2 * sizeof(float) + 255) / 256 * 256;
   }
 };
+
+// The checks and arguments that the attentions share, once the descriptor is checked.
+ss_status prepare_attend(ss::CacheAttendArgs *p, const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const void *q,
+                         int64_t q_row_stride, int32_t num_rows, const int32_t *row_start, const int32_t *end, float *out, float *lse,
+                         const float *prev_out, const float *prev_lse, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  const int64_t packed = (int64_t)desc->num_q_heads * ss::kCacheDim;
+  if (q == nullptr || out == nullptr || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4))
+    return fail(SS_ERR_INVALID_ARGUMENT, "q and out must be non-null and 16-byte aligned, lse null or 4-byte aligned");
+  if (q_row_stride != 0 && (q_row_stride < packed || q_row_stride % 8 != 0))
+    return fail(SS_ERR_INVALID_ARGUMENT, "q_row_stride must be 0 or a multiple of 8 of at least %lld elements (got %lld)",
+                (long long)packed, (long long)q_row_stride);
+  if ((prev_out == nullptr) != (prev_lse == nullptr))
+    return fail(SS_ERR_INVALID_ARGUMENT, "prev_out and prev_lse come together");
+  if (!aligned(prev_out, 16) || !aligned(prev_lse, 4))
+    return fail(SS_ERR_INVALID_ARGUMENT, "prev_out must be 16-byte and prev_lse 4-byte aligned");
+  const AttendLayout layout(desc);
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layout.bytes)
+    return fail(SS_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold %zu bytes (got %p, %zu)", layout.bytes, workspace,
+                workspace_bytes);
+  const ss_status s = check_call(desc, pages, page_table, num_rows, row_start, end, stream);
+  if (s != SS_OK) return s;
+  fill(p, desc, pages, page_table, num_rows, row_start, end);
+  p->q = static_cast<const uint16_t *>(q);
+  p->q_row_stride = q_row_stride != 0 ? q_row_stride : packed;
+  p->out = out;
+  p->lse = lse;
+  p->prev_out = prev_out;
+  p->prev_lse = prev_lse;
+  p->part_a = static_cast<float *>(workspace);
+  p->part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + layout.ml);
+  p->Hq = desc->num_q_heads;
+  p->G = desc->num_q_heads / desc->num_kv_heads;
+  p->g_inv = (65536u + (uint32_t)p->G - 1) / (uint32_t)p->G;
+  p->M = layout.M;
+  p->workers = layout.split.workers;
+  p->alone = layout.split.alone;
+  p->piece_units = layout.split.piece_units;
+  p->causal = desc->causal;
+  p->scale_log2 = desc->softmax_scale * kLog2e;
+  return SS_OK;
+}
 
 }  // namespace
 
@@ -201,43 +268,138 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
                           size_t workspace_bytes, hipStream_t stream) {
   ss_status s = check_attend_desc(desc);
   if (s != SS_OK) return s;
-  const int64_t packed = (int64_t)desc->num_q_heads * ss::kCacheDim;
-  if (q == nullptr || out == nullptr || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4))
-    return fail(SS_ERR_INVALID_ARGUMENT, "q and out must be non-null and 16-byte aligned, lse null or 4-byte aligned");
-  if (q_row_stride != 0 && (q_row_stride < packed || q_row_stride % 8 != 0))
-    return fail(SS_ERR_INVALID_ARGUMENT, "q_row_stride must be 0 or a multiple of 8 of at least %lld elements (got %lld)",
-                (long long)packed, (long long)q_row_stride);
-  if ((prev_out == nullptr) != (prev_lse == nullptr))
-    return fail(SS_ERR_INVALID_ARGUMENT, "prev_out and prev_lse come together");
-  if (!aligned(prev_out, 16) || !aligned(prev_lse, 4))
-    return fail(SS_ERR_INVALID_ARGUMENT, "prev_out must be 16-byte and prev_lse 4-byte aligned");
-  const AttendLayout layout(desc);
-  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layout.bytes)
-    return fail(SS_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold %zu bytes (got %p, %zu)", layout.bytes, workspace,
-                workspace_bytes);
-  s = check_call(desc, pages, page_table, num_rows, row_start, end, stream);
-  if (s != SS_OK) return s;
   ss::CacheAttendArgs p;
-  fill(&p, desc, pages, page_table, num_rows, row_start, end);
-  p.q = static_cast<const uint16_t *>(q);
-  p.q_row_stride = q_row_stride != 0 ? q_row_stride : packed;
-  p.out = out;
-  p.lse = lse;
-  p.prev_out = prev_out;
-  p.prev_lse = prev_lse;
-  p.part_a = static_cast<float *>(workspace);
-  p.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + layout.ml);
-  p.Hq = desc->num_q_heads;
-  p.G = desc->num_q_heads / desc->num_kv_heads;
-  p.g_inv = (65536u + (uint32_t)p.G - 1) / (uint32_t)p.G;
-  p.M = layout.M;
-  p.workers = layout.split.workers;
-  p.alone = layout.split.alone;
-  p.piece_units = layout.split.piece_units;
-  p.causal = desc->causal;
-  p.scale_log2 = desc->softmax_scale * kLog2e;
+  s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
+                     workspace_bytes, stream);
+  if (s != SS_OK) return s;
   const hipError_t e = ss::launch_cache_attend(p, desc->format, stream);
   return e == hipSuccess ? SS_OK : hip_fail(e, "cache attention launch");
+}
+
+size_t ss_cache_attend_tree_workspace_bytes(const ss_cache_desc *desc) {
+  if (check_tree_desc(desc) != SS_OK) return 0;
+  return AttendLayout(desc).bytes;
+}
+
+ss_status ss_cache_attend_tree(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const uint64_t *tree,
+                               int32_t window, int32_t sinks, const void *q, int64_t q_row_stride, int32_t num_rows,
+                               const int32_t *row_start, const int32_t *end, float *out, float *lse, const float *prev_out,
+                               const float *prev_lse, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  ss_status s = check_tree_desc(desc);
+  if (s != SS_OK) return s;
+  if (tree == nullptr || !aligned(tree, 8)) return fail(SS_ERR_INVALID_ARGUMENT, "tree must be non-null and 8-byte aligned");
+  s = check_window(window, sinks, 0);
+  if (s != SS_OK) return s;
+  ss::CacheSeenArgs p;
+  s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
+                     workspace_bytes, stream);
+  if (s != SS_OK) return s;
+  p.tree = tree;
+  p.window = window;
+  p.sinks = sinks;
+  const hipError_t e = ss::launch_cache_attend_seen(p, desc->format, stream);
+  return e == hipSuccess ? SS_OK : hip_fail(e, "cache tree attention launch");
+}
+
+ss_status ss_cache_attend_window(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, int32_t window,
+                                 int32_t sinks, const void *q, int64_t q_row_stride, int32_t num_rows, const int32_t *row_start,
+                                 const int32_t *end, float *out, float *lse, const float *prev_out, const float *prev_lse,
+                                 void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  ss_status s = check_attend_desc(desc);
+  if (s != SS_OK) return s;
+  if (desc->causal != 1) return fail(SS_ERR_INVALID_ARGUMENT, "a window takes causal = 1");
+  s = check_window(window, sinks, 1);
+  if (s != SS_OK) return s;
+  ss::CacheSeenArgs p;
+  s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
+                     workspace_bytes, stream);
+  if (s != SS_OK) return s;
+  p.tree = nullptr;
+  p.window = window;
+  p.sinks = sinks;
+  const hipError_t e = ss::launch_cache_attend_seen(p, desc->format, stream);
+  return e == hipSuccess ? SS_OK : hip_fail(e, "cache window attention launch");
+}
+
+ss_status ss_cache_append(const ss_cache_desc *desc, void *pages, const int32_t *page_table, const ss_rope_desc *rope,
+                          const int32_t *positions, const void *k, const void *v, int64_t row_stride, const void *q,
+                          int64_t q_row_stride, void *q_out, int64_t q_out_row_stride, int32_t num_rows,
+                          const int32_t *row_start, const int32_t *end, hipStream_t stream) {
+  ss_status s = check_desc(desc);
+  if (s != SS_OK) return s;
+  if (rope == nullptr) return fail(SS_ERR_INVALID_ARGUMENT, "rope descriptor is null");
+  if (rope->rotary_dim < 1 || rope->rotary_dim > ss::kCacheDim)
+    return fail(SS_ERR_INVALID_ARGUMENT, "rotary_dim must be 1..%d (got %d)", ss::kCacheDim, rope->rotary_dim);
+  if (rope->rotary_dim % 16 != 0) return fail(SS_ERR_UNSUPPORTED, "rotary_dim %d is not built (only multiples of 16)", rope->rotary_dim);
+  if (rope->interleaved != 0 && rope->interleaved != 1)
+    return fail(SS_ERR_INVALID_ARGUMENT, "interleaved must be 0 or 1 (got %d)", rope->interleaved);
+  if (!(rope->scale > 0.f) || !std::isfinite(rope->scale))
+    return fail(SS_ERR_INVALID_ARGUMENT, "rope scale must be positive and finite (got %g)", (double)rope->scale);
+  if (rope->inv_freq == nullptr || !aligned(rope->inv_freq, 4) || !aligned(positions, 4))
+    return fail(SS_ERR_INVALID_ARGUMENT, "inv_freq must be non-null, it and positions 4-byte aligned");
+  const int64_t packed = (int64_t)desc->num_kv_heads * ss::kCacheDim;
+  if (k == nullptr || v == nullptr || !aligned(k, 16) || !aligned(v, 16))
+    return fail(SS_ERR_INVALID_ARGUMENT, "k and v must be non-null and 16-byte aligned");
+  if (row_stride != 0 && (row_stride < packed || row_stride % 8 != 0))
+    return fail(SS_ERR_INVALID_ARGUMENT, "row_stride must be 0 or a multiple of 8 of at least %lld elements (got %lld)",
+                (long long)packed, (long long)row_stride);
+  if ((q == nullptr) != (q_out == nullptr)) return fail(SS_ERR_INVALID_ARGUMENT, "q and q_out come together");
+  int64_t q_packed = 0;
+  if (q != nullptr) {
+    if (!aligned(q, 16) || !aligned(q_out, 16)) return fail(SS_ERR_INVALID_ARGUMENT, "q and q_out must be 16-byte aligned");
+    if (desc->num_q_heads < 1 || desc->num_q_heads % desc->num_kv_heads != 0)
+      return fail(SS_ERR_INVALID_ARGUMENT, "num_q_heads must be a positive multiple of num_kv_heads (got %d, %d)", desc->num_q_heads,
+                  desc->num_kv_heads);
+    // a launch's grid has a workgroup for every two query heads, at most
+    if (desc->num_q_heads > 65536) return fail(SS_ERR_UNSUPPORTED, "num_q_heads %d > 65536", desc->num_q_heads);
+    q_packed = (int64_t)desc->num_q_heads * ss::kCacheDim;
+    for (const int64_t stride : {q_row_stride, q_out_row_stride})
+      if (stride != 0 && (stride < q_packed || stride % 8 != 0))
+        return fail(SS_ERR_INVALID_ARGUMENT, "q_row_stride and q_out_row_stride must be 0 or a multiple of 8 of at least %lld elements (got %lld)",
+                    (long long)q_packed, (long long)stride);
+    if (q == q_out && (q_row_stride != 0 ? q_row_stride : q_packed) != (q_out_row_stride != 0 ? q_out_row_stride : q_packed))
+      return fail(SS_ERR_INVALID_ARGUMENT, "q_out may be q with the same row stride only");
+  }
+  s = check_rows(num_rows);
+  if (s != SS_OK) return s;
+  s = check_call(desc, pages, page_table, num_rows, row_start, end, stream);
+  if (s != SS_OK) return s;
+  ss::CacheAppendArgs p;
+  fill(&p, desc, pages, page_table, num_rows, row_start, end);
+  p.k = static_cast<const uint16_t *>(k);
+  p.v = static_cast<const uint16_t *>(v);
+  p.q = static_cast<const uint16_t *>(q);
+  p.q_out = static_cast<uint16_t *>(q_out);
+  p.row_stride = row_stride != 0 ? row_stride : packed;
+  p.q_row_stride = q_row_stride != 0 ? q_row_stride : q_packed;
+  p.q_out_row_stride = q_out_row_stride != 0 ? q_out_row_stride : q_packed;
+  p.positions = positions;
+  p.inv_freq = rope->inv_freq;
+  p.scale = rope->scale;
+  p.Hq = desc->num_q_heads;
+  p.rotary_dim = rope->rotary_dim;
+  p.interleaved = rope->interleaved;
+  const hipError_t e = ss::launch_cache_append(p, desc->format, stream);
+  return e == hipSuccess ? SS_OK : hip_fail(e, "cache append launch");
+}
+
+ss_status ss_cache_keep(const ss_cache_desc *desc, void *pages, const int32_t *page_table, const int32_t *kept,
+                        const int32_t *num_kept, int32_t num_rows, const int32_t *row_start, const int32_t *end,
+                        hipStream_t stream) {
+  ss_status s = check_desc(desc);
+  if (s != SS_OK) return s;
+  if (desc->max_rows > SS_CACHE_MAX_TREE)
+    return fail(SS_ERR_INVALID_ARGUMENT, "max_rows must be at most %d to keep a path (got %d)", SS_CACHE_MAX_TREE, desc->max_rows);
+  if (kept == nullptr || num_kept == nullptr || !aligned(kept, 4) || !aligned(num_kept, 4))
+    return fail(SS_ERR_INVALID_ARGUMENT, "kept and num_kept must be non-null and 4-byte aligned");
+  s = check_call(desc, pages, page_table, num_rows, row_start, end, stream);
+  if (s != SS_OK) return s;
+  ss::CacheKeepArgs p;
+  fill(&p, desc, pages, page_table, num_rows, row_start, end);
+  p.kept = kept;
+  p.num_kept = num_kept;
+  const hipError_t e = ss::launch_cache_keep(p, desc->format, stream);
+  return e == hipSuccess ? SS_OK : hip_fail(e, "cache keep launch");
 }
 
 }  // extern "C"

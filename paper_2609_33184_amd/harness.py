@@ -5,8 +5,9 @@ of the round runs in libspecstream's kernels through the binding.
 """
 from __future__ import annotations
 
+import itertools
 import operator
-from typing import Dict, List, Optional, Sequence, Tuple
+from typing import Callable, Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -333,17 +334,27 @@ class PagedCache:
     What calls on several streams write and read in the same pages is the
     caller's to order, and so are a captured call's replays: behind the changes
     that they need, never beside a change or another attention.  One host
-    thread uses a cache at a time."""
+    thread uses a cache at a time.
+
+    ``tree_rows``: most nodes of a request's tree of drafted tokens (0: none).
+    A step with trees is ``grow``, ``append`` (or ``write``), ``attend_tree``
+    and ``keep``."""
 
     def __init__(self, num_requests: int, num_q_heads: int, num_kv_heads: int, max_tokens: int, fmt: int = ss.SS_CACHE_MXFP8,
                  page_tokens: int = 64, num_pages: Optional[int] = None, max_rows: int = 1,
-                 softmax_scale: Optional[float] = None, causal: int = 1, device="cuda"):
+                 softmax_scale: Optional[float] = None, causal: int = 1, device="cuda", tree_rows: int = 0):
         width = -(-max_tokens // page_tokens)
         pages = num_requests * width if num_pages is None else num_pages
         self.desc = ss.make_cache_desc(num_requests, num_kv_heads, fmt, page_tokens, pages, width, num_q_heads,
                                        max_rows=max_rows, softmax_scale=softmax_scale, causal=causal)
         page_bytes = ss.ss_cache_page_bytes(self.desc)
         ws_bytes = ss.ss_cache_attend_workspace_bytes(self.desc)
+        self.tree_desc: Optional[ss.ss_cache_desc] = None
+        if tree_rows != 0 and ws_bytes != 0:
+            self.tree_desc = ss.make_cache_desc(num_requests, num_kv_heads, fmt, page_tokens, pages, width, num_q_heads,
+                                                max_rows=tree_rows, softmax_scale=softmax_scale, causal=causal)
+            tree_bytes = ss.ss_cache_attend_tree_workspace_bytes(self.tree_desc)
+            ws_bytes = max(ws_bytes, tree_bytes) if tree_bytes else 0
         if page_bytes == 0 or ws_bytes == 0:
             raise ss.SpecStreamError(ss.SS_ERR_INVALID_ARGUMENT, "PagedCache", ss.ss_last_error())
         self.pages = torch.empty(pages, num_kv_heads, page_bytes // num_kv_heads, dtype=torch.uint8, device=device)
@@ -363,13 +374,18 @@ class PagedCache:
             raise RuntimeError("grow and release change the host's counts too: they cannot be captured")
         return rows
 
-    def _post(self, rows: List[int], places: List[int], ids: List[int]) -> None:
-        """``end`` and table entries change on torch's current stream.  The numbers travel in one copy from pinned
-        memory, which torch hands out again only once that copy is done, so that the host waits for nothing."""
-        x = torch.tensor(rows + places + ids, dtype=torch.int32)
+    def _post(self, rows: List[int], places: List[int], ids: List[int], more: Sequence[int] = (),
+              first: Optional[Callable[[torch.Tensor], None]] = None) -> None:
+        """``end`` and table entries change on torch's current stream, once ``first`` was called with ``more`` there.
+        The numbers travel in one copy from pinned memory, which torch hands out again only once that copy is done, so
+        that the host waits for nothing."""
+        x = torch.tensor([*more, *rows, *places, *ids], dtype=torch.int32)
         if self.order is not None:
             x = x.pin_memory().to(self.end.device, non_blocking=True)
             self.order.change_begins()
+        if first is not None:
+            first(x[:len(more)])
+        x = x[len(more):]
         n, m = len(rows), len(rows) + len(places)
         if ids:
             self.table.view(-1)[x[n:m]] = x[m:]
@@ -402,15 +418,48 @@ class PagedCache:
         rows = self._counts(rows)
         if any(n > t for n, t in zip(rows, self.tokens)):
             raise ValueError(f"a request holds fewer tokens than it is to release (holds {self.tokens}, releases {rows})")
+        self._release(rows)
+
+    def _release(self, rows: List[int], more: Sequence[int] = (), first: Optional[Callable[[torch.Tensor], None]] = None) -> None:
         keep = [-(-(t - n) // self.desc.page_tokens) for n, t in zip(rows, self.tokens)]
         places: List[int] = []
         for b, k in enumerate(keep):
             places += range(b * self.table.shape[1] + k, b * self.table.shape[1] + len(self.owned[b]))
-        self._post([-n for n in rows], places, [-1] * len(places))
+        self._post([-n for n in rows], places, [-1] * len(places), more, first)
         for b, n in enumerate(rows):
             self.tokens[b] -= n
             self.free += self.owned[b][keep[b]:]
             del self.owned[b][keep[b]:]
+
+    def keep(self, kept: Sequence[Sequence[int]], rows: Sequence[int]) -> None:
+        """Of request b's last rows[b] tokens, a tree's nodes, those numbered kept[b] stay, in that order, behind the
+        history; the others are released.  A change like ``grow`` and ``release``, on torch's current stream."""
+        desc = self._tree()
+        rows = self._counts(rows)
+        paths = [[operator.index(i) for i in path] for path in kept]
+        if len(paths) != len(rows):
+            raise ValueError(f"one path for each of {len(rows)} requests (got {len(paths)})")
+        for path, n, tokens in zip(paths, rows, self.tokens):
+            if n > min(tokens, desc.max_rows) or len(path) > n or any(not 0 <= i < n for i in path):
+                raise ValueError(f"a path is at most a tree's nodes, a tree at most {desc.max_rows} of a request's tokens "
+                                 f"(got {path} of {n} nodes, {tokens} tokens)")
+        starts = [0, *itertools.accumulate(rows)]
+        total, B = starts[-1], len(rows)
+        listed = [i for path, n in zip(paths, rows) for i in path + [-1] * (n - len(path))]
+
+        def move(x: torch.Tensor) -> None:
+            ss.ss_cache_keep(desc, self.pages.data_ptr(), self.table.data_ptr(), x[2 * B + 1:].data_ptr(), x.data_ptr(), total,
+                             self.end.data_ptr(), x[B:].data_ptr(), torch.cuda.current_stream(self.pages.device).cuda_stream)
+
+        moves = total > 0 and any(path != list(range(len(path))) for path in paths)
+        if moves:
+            self._on_current_device()
+        self._release([n - len(path) for path, n in zip(paths, rows)], [*map(len, paths), *starts, *listed], move if moves else None)
+
+    def _tree(self) -> ss.ss_cache_desc:
+        if self.tree_desc is None:
+            raise ValueError("a cache made without tree_rows has no trees")
+        return self.tree_desc
 
     def _on_current_device(self) -> None:
         """A call runs on the current device, wherever its addresses lead."""
@@ -464,6 +513,35 @@ class PagedCache:
         if on is not None:
             self.order.call_ends(on, False)
 
+    def append(self, k: torch.Tensor, v: torch.Tensor, inv_freq: torch.Tensor, stream: int,
+               row_start: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, interleaved: int = 0,
+               scale: float = 1.0) -> None:
+        """Rows enter as in ``write``, K turned by their positions (the tokens' own, or int32 [T]); so do rows q [T, Hq,
+        128] into q_out (which may be q).  inv_freq: fp32, one for each of the pairs of channels that turn."""
+        stride = self._row_stride(k, self.desc.num_kv_heads)
+        if v.shape != k.shape or self._row_stride(v, self.desc.num_kv_heads) != stride:
+            raise ValueError(f"k and v have one shape and one row stride (got {list(k.shape)} {k.stride()}, {list(v.shape)} {v.stride()})")
+        if (not isinstance(inv_freq, torch.Tensor) or inv_freq.dtype != torch.float32 or inv_freq.dim() != 1
+                or not inv_freq.is_contiguous() or inv_freq.device != self.pages.device):
+            raise ValueError(f"inv_freq is a packed fp32 tensor on {self.pages.device}")
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out come together")
+        q_strides = [0, 0]
+        if q is not None:
+            q_strides = [self._row_stride(x, self.desc.num_q_heads) for x in (q, q_out)]
+            if q.shape != q_out.shape or q.shape[0] != k.shape[0]:
+                raise ValueError(f"q and q_out have k's {k.shape[0]} rows (got {list(q.shape)}, {list(q_out.shape)})")
+        at = None if positions is None else self._counters(positions, k.shape[0], "positions")
+        starts = self._starts(row_start)
+        rope = ss.make_rope_desc(2 * inv_freq.numel(), inv_freq.data_ptr(), interleaved, scale)
+        on = self._begins(stream, False)
+        ss.ss_cache_append(self.desc, self.pages.data_ptr(), self.table.data_ptr(), rope, k.data_ptr(), v.data_ptr(), k.shape[0],
+                           self.end.data_ptr(), starts, stride, at, None if q is None else q.data_ptr(),
+                           None if q_out is None else q_out.data_ptr(), *q_strides, stream)
+        if on is not None:
+            self.order.call_ends(on, False)
+
     def _chunk(self, k: torch.Tensor, v: torch.Tensor, num_rows: int, kv_layout: int) -> None:
         """k and v hold num_rows tokens in the given layout: packed, or the views of one chunk of K and V rows."""
         heads, d = self.desc.num_kv_heads, self.desc.head_dim
@@ -496,20 +574,55 @@ class PagedCache:
         if on is not None:
             self.order.call_ends(on, False)
 
-    def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
-               row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
-        """out, lse of rows q [T, Hq, 128], joined with ``prev``'s if given."""
-        stride = self._row_stride(q, self.desc.num_q_heads)
+    def _results(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
+                 prev: Optional[Tuple[torch.Tensor, torch.Tensor]]) -> Tuple[Optional[int], ...]:
+        """Addresses of out, lse and prev's, as the attentions take them."""
         for x, shape in ((out, q.shape), (lse, q.shape[:2])) + (((prev[0], q.shape), (prev[1], q.shape[:2])) if prev else ()):
             if x is not None and (x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.device != q.device):
                 raise ValueError(f"out, lse and prev are packed fp32 {list(q.shape)}, {list(q.shape[:2])} on {q.device} "
                                  f"(got {x.dtype} {list(x.shape)} on {x.device})")
+        return (out.data_ptr(), None if lse is None else lse.data_ptr(), None if prev is None else prev[0].data_ptr(),
+                None if prev is None else prev[1].data_ptr())
+
+    def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
+               row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+               window: int = 0, sinks: int = 0) -> None:
+        """out, lse of rows q [T, Hq, 128], joined with ``prev``'s if given.  window > 0: a row sees the last ``window``
+        tokens up to its own, and the request's first ``sinks``."""
+        stride = self._row_stride(q, self.desc.num_q_heads)
+        to, to_lse, prev_out, prev_lse = self._results(q, out, lse, prev)
         starts = self._starts(row_start)
+        if window < 0 or sinks < 0 or sinks > 0 and window == 0:
+            raise ValueError(f"window and sinks are 0 or more, sinks with a window only (got {window}, {sinks})")
         on = self._begins(stream, True)
-        ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
-                           self.end.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-                           starts, None if prev is None else prev[0].data_ptr(),
-                           None if prev is None else prev[1].data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
-                           stride, stream)
+        if window == 0:
+            ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
+                               self.end.data_ptr(), to, to_lse, starts, prev_out, prev_lse, self.workspace.data_ptr(),
+                               self.workspace.numel(), stride, stream)
+        else:
+            ss.ss_cache_attend_window(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
+                                      self.end.data_ptr(), to, window, sinks, to_lse, starts, prev_out, prev_lse,
+                                      self.workspace.data_ptr(), self.workspace.numel(), stride, stream)
+        if on is not None:
+            self.order.call_ends(on, True)
+
+    def attend_tree(self, q: torch.Tensor, tree: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
+                    row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                    window: int = 0, sinks: int = 0) -> None:
+        """out, lse of rows q [T, Hq, 128], each request's last tokens a tree: bit j of tree[row] (int64 or uint64 [T])
+        stands for the request's j-th row's token.  The window is one on the tokens before the tree."""
+        desc = self._tree()
+        stride = self._row_stride(q, self.desc.num_q_heads)
+        if (not isinstance(tree, torch.Tensor) or tree.dtype not in (torch.int64, torch.uint64) or tree.shape != q.shape[:1]
+                or not tree.is_contiguous() or tree.device != self.pages.device):
+            raise ValueError(f"tree is a packed int64 or uint64 [{q.shape[0]}] on {self.pages.device}")
+        to, to_lse, prev_out, prev_lse = self._results(q, out, lse, prev)
+        starts = self._starts(row_start)
+        if window < 0 or sinks < 0 or sinks > 0 and window == 0:
+            raise ValueError(f"window and sinks are 0 or more, sinks with a window only (got {window}, {sinks})")
+        on = self._begins(stream, True)
+        ss.ss_cache_attend_tree(desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0], self.end.data_ptr(),
+                                tree.data_ptr(), to, to_lse, starts, window, sinks, prev_out, prev_lse,
+                                self.workspace.data_ptr(), self.workspace.numel(), stride, stream)
         if on is not None:
             self.order.call_ends(on, True)

@@ -45,6 +45,7 @@ EXPORTED = (
     "ss_tier_endpoint", "ss_tier_create", "ss_tier_destroy", "ss_tier_get", "ss_tier_extend", "ss_tier_commit",
     "ss_tier_plan", "ss_tier_complete", "ss_download_range",
     "ss_cache_page_bytes", "ss_cache_write", "ss_cache_read", "ss_cache_attend_workspace_bytes", "ss_cache_attend",
+    "ss_cache_attend_window", "ss_cache_append", "ss_cache_attend_tree_workspace_bytes", "ss_cache_attend_tree", "ss_cache_keep",
     "ss_width_create", "ss_width_destroy", "ss_width_observe", "ss_width_select", "ss_width_estimate",
 )
 
@@ -111,6 +112,20 @@ def make_cache_desc(num_requests: int, num_kv_heads: int, format: int, page_toke
                          page_stride, max_rows, (head_dim ** -0.5) if softmax_scale is None else softmax_scale, causal)
 
 
+class ss_rope_desc(ctypes.Structure):
+    _fields_ = [
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("inv_freq", ctypes.c_void_p),
+    ]
+
+
+def make_rope_desc(rotary_dim: int, inv_freq: int, interleaved: int = 0, scale: float = 1.0) -> ss_rope_desc:
+    """Build a descriptor of how rows are turned by their positions (inv_freq: device address of fp32 [rotary_dim / 2])."""
+    return ss_rope_desc(rotary_dim, interleaved, scale, inv_freq)
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -160,6 +175,12 @@ def load() -> ctypes.CDLL:
         "ss_cache_read": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, P, I32, I32, P, P, P]),
         "ss_cache_attend_workspace_bytes": (SZ, [ctypes.POINTER(ss_cache_desc)]),
         "ss_cache_attend": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, I64, I32, P, P, P, P, P, P, P, SZ, P]),
+        "ss_cache_attend_window": (I32, [ctypes.POINTER(ss_cache_desc), P, P, I32, I32, P, I64, I32, P, P, P, P, P, P, P, SZ, P]),
+        "ss_cache_append": (I32, [ctypes.POINTER(ss_cache_desc), P, P, ctypes.POINTER(ss_rope_desc), P, P, P, I64, P, I64, P, I64, I32,
+                                  P, P, P]),
+        "ss_cache_attend_tree_workspace_bytes": (SZ, [ctypes.POINTER(ss_cache_desc)]),
+        "ss_cache_attend_tree": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, I32, I32, P, I64, I32, P, P, P, P, P, P, P, SZ, P]),
+        "ss_cache_keep": (I32, [ctypes.POINTER(ss_cache_desc), P, P, P, P, I32, P, P, P]),
         "ss_width_create": (I32, [ctypes.POINTER(P), PI32, I32, D, I32, D]),
         "ss_width_destroy": (None, [P]),
         "ss_width_observe": (I32, [P, I32, D, D, D, D, D]),
@@ -375,6 +396,42 @@ def ss_cache_attend(desc: ss_cache_desc, pages: int, page_table: int, q: int, nu
                     stream: int = 0) -> None:
     _check(load().ss_cache_attend(ctypes.byref(desc), pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse,
                                   prev_out, prev_lse, workspace, workspace_bytes, stream), "ss_cache_attend")
+
+
+def ss_cache_attend_window(desc: ss_cache_desc, pages: int, page_table: int, q: int, num_rows: int, end: int, out: int,
+                           window: int, sinks: int = 0, lse: Optional[int] = None, row_start: Optional[int] = None,
+                           prev_out: Optional[int] = None, prev_lse: Optional[int] = None, workspace: int = 0,
+                           workspace_bytes: int = 0, q_row_stride: int = 0, stream: int = 0) -> None:
+    _check(load().ss_cache_attend_window(ctypes.byref(desc), pages, page_table, window, sinks, q, q_row_stride, num_rows, row_start,
+                                         end, out, lse, prev_out, prev_lse, workspace, workspace_bytes, stream),
+           "ss_cache_attend_window")
+
+
+def ss_cache_append(desc: ss_cache_desc, pages: int, page_table: int, rope: ss_rope_desc, k: int, v: int, num_rows: int, end: int,
+                    row_start: Optional[int] = None, row_stride: int = 0, positions: Optional[int] = None,
+                    q: Optional[int] = None, q_out: Optional[int] = None, q_row_stride: int = 0, q_out_row_stride: int = 0,
+                    stream: int = 0) -> None:
+    _check(load().ss_cache_append(ctypes.byref(desc), pages, page_table, ctypes.byref(rope), positions, k, v, row_stride, q,
+                                  q_row_stride, q_out, q_out_row_stride, num_rows, row_start, end, stream), "ss_cache_append")
+
+
+def ss_cache_attend_tree_workspace_bytes(desc: ss_cache_desc) -> int:
+    return int(load().ss_cache_attend_tree_workspace_bytes(ctypes.byref(desc)))
+
+
+def ss_cache_attend_tree(desc: ss_cache_desc, pages: int, page_table: int, q: int, num_rows: int, end: int, tree: int, out: int,
+                         lse: Optional[int] = None, row_start: Optional[int] = None, window: int = 0, sinks: int = 0,
+                         prev_out: Optional[int] = None, prev_lse: Optional[int] = None, workspace: int = 0,
+                         workspace_bytes: int = 0, q_row_stride: int = 0, stream: int = 0) -> None:
+    _check(load().ss_cache_attend_tree(ctypes.byref(desc), pages, page_table, tree, window, sinks, q, q_row_stride, num_rows,
+                                       row_start, end, out, lse, prev_out, prev_lse, workspace, workspace_bytes, stream),
+           "ss_cache_attend_tree")
+
+
+def ss_cache_keep(desc: ss_cache_desc, pages: int, page_table: int, kept: int, num_kept: int, num_rows: int, end: int,
+                  row_start: Optional[int] = None, stream: int = 0) -> None:
+    _check(load().ss_cache_keep(ctypes.byref(desc), pages, page_table, kept, num_kept, num_rows, row_start, end, stream),
+           "ss_cache_keep")
 
 
 # ---------------------------------------------------------------------------
