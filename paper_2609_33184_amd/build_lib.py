@@ -31,7 +31,7 @@ def build(verbose: bool = True) -> str:
     bdir = os.path.join(ROOT, "_build")
     os.makedirs(bdir, exist_ok=True)
     objs = []
-    for name in ("ss_kernels", "ss_copy", "ss_cache", "ss_cache_append"):
+    for name in ("ss_kernels", "ss_copy", "ss_cache", "ss_cache_append", "ss_cache_group"):
         kobj = os.path.join(bdir, name + ".o")
         _run([HIPCC, *COMMON, *DEVICE_ONLY, "-c", os.path.join(CSRC, name + ".hip"), "-o", kobj])
         objs.append(kobj)

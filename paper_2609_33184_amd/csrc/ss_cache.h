@@ -77,6 +77,8 @@ struct CacheAttendArgs : CacheArgs {
 // Rows of one KV head that a piece of the attention below holds at most: more are
 // attended in blocks of as many.
 constexpr int kCacheRowBlock = 64;
+// And of the attention of many rows, with the tokens of its tiles.
+constexpr int kCacheGroupBlock = 128, kCacheGroupTile = 32;
 
 // Rows that see a tree, or a window and the first tokens, instead of a chain.
 struct CacheSeenArgs : CacheAttendArgs {
@@ -85,6 +87,8 @@ struct CacheSeenArgs : CacheAttendArgs {
   int32_t sinks;          // first tokens that it sees as well
 };
 
+struct CacheGroupArgs : CacheSeenArgs {};
+
 // How the attention over a cache of this kind is split; M query rows per KV head.
 struct CacheSplit {
   int workers;
@@ -92,6 +96,9 @@ struct CacheSplit {
   int piece_units;
 };
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
+// From how many rows per KV head on the rows of a tree are attended in groups, and how that is split.
+constexpr int kCacheGroupRows = 65;
+CacheSplit cache_group_split(int fmt, int B, int Hkv, int capacity, int M);
 inline int cache_row_blocks(int M) { return (M + kCacheRowBlock - 1) / kCacheRowBlock; }
 
 // Launch wrappers; return hipGetLastError() of the launch.
@@ -101,5 +108,6 @@ hipError_t launch_cache_attend(const CacheAttendArgs &p, int fmt, hipStream_t s)
 hipError_t launch_cache_append(const CacheAppendArgs &p, int fmt, hipStream_t s);
 hipError_t launch_cache_keep(const CacheKeepArgs &p, int fmt, hipStream_t s);
 hipError_t launch_cache_attend_seen(const CacheSeenArgs &p, int fmt, hipStream_t s);
+hipError_t launch_cache_attend_group(const CacheGroupArgs &p, int fmt, hipStream_t s);
 
 }  // namespace ss

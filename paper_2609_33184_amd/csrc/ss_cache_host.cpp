@@ -145,12 +145,16 @@ void fill(ss::CacheArgs *p, const ss_cache_desc *d, const void *pages, const int
 
 struct AttendLayout {
   int M;
+  bool group;         // attended by the kernel of many rows
   ss::CacheSplit split;
   size_t ml, bytes;   // offset of the maxima and sums; all of it
   explicit AttendLayout(const ss_cache_desc *d) {
     M = d->max_rows * (d->num_q_heads / d->num_kv_heads);
-    split = ss::cache_attend_split(d->format, d->num_requests, d->num_kv_heads, d->table_stride * d->page_tokens, M);
-    const size_t rows = 2 * (size_t)split.workers * (size_t)(M < ss::kCacheRowBlock ? M : ss::kCacheRowBlock);
+    group = M >= ss::kCacheGroupRows;
+    const int reach = d->table_stride * d->page_tokens, block = group ? ss::kCacheGroupBlock : ss::kCacheRowBlock;
+    split = group ? ss::cache_group_split(d->format, d->num_requests, d->num_kv_heads, reach, M)
+                  : ss::cache_attend_split(d->format, d->num_requests, d->num_kv_heads, reach, M);
+    const size_t rows = 2 * (size_t)split.workers * (size_t)(M < block ? M : block);
     ml = rows * ss::kCacheDim * sizeof(float);
     bytes = (ml + rows * 2 * sizeof(float) + 255) / 256 * 256;
   }
@@ -290,14 +294,15 @@ ss_status ss_cache_attend_tree(const ss_cache_desc *desc, const void *pages, con
   if (tree == nullptr || !aligned(tree, 8)) return fail(SS_ERR_INVALID_ARGUMENT, "tree must be non-null and 8-byte aligned");
   s = check_window(window, sinks, 0);
   if (s != SS_OK) return s;
-  ss::CacheSeenArgs p;
+  ss::CacheGroupArgs p;
   s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
                      workspace_bytes, stream);
   if (s != SS_OK) return s;
   p.tree = tree;
   p.window = window;
   p.sinks = sinks;
-  const hipError_t e = ss::launch_cache_attend_seen(p, desc->format, stream);
+  const hipError_t e = AttendLayout(desc).group ? ss::launch_cache_attend_group(p, desc->format, stream)
+                                                : ss::launch_cache_attend_seen(p, desc->format, stream);
   return e == hipSuccess ? SS_OK : hip_fail(e, "cache tree attention launch");
 }
 

@@ -359,6 +359,33 @@ def test_tree_joined_without_row_start_and_repeats():
     assert torch.equal(first, r.out) and torch.equal(fl, r.lse)
 
 
+@pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
+@pytest.mark.parametrize("hq,n", ((8, 7), (8, 40), (16, 64)))
+@pytest.mark.parametrize("factor", (2.0 ** 14, 2.0 ** -40, 0.0))
+def test_tree_values_of_every_size(fmt, hq, n, factor):
+    """Values far above and below the others, and zeros, in history tiles, in the tree's, in all tokens."""
+    rng = np.random.default_rng(n)
+    end = [400 + n, 70 + n, n]
+    v = _normal(6, sum(end), 2, 128)
+    v[100:133, 0] *= factor
+    v[200, 1, 32:64] *= factor
+    v[end[0] - 3:end[0], 1] *= factor
+    v[end[0]:end[0] + end[1]] *= factor
+    c = Cache(fmt, 2, 32, end)
+    c.fill_tokens(end, 5, v=v)
+    r = TreeRows(c, hq, _trees(rng, (n, n, n)), end).run()
+    torch.cuda.synchronize()
+    want, wl = r.want()
+    got = r.out.cpu().numpy().astype(np.float64)
+    # a value's error is relative to the largest |v| of its request, head and channel block: a weighted mean's weights are off by 5e-6 in the 2-norm
+    for b in range(3):
+        mine = slice(n * b, n * (b + 1))
+        for h in range(2):
+            g, x = got[mine, h * hq // 2:(h + 1) * hq // 2], want[mine, h * hq // 2:(h + 1) * hq // 2]
+            assert np.linalg.norm(g - x) <= 5e-6 * np.linalg.norm(x)
+    assert np.abs(r.lse.cpu().numpy() - wl).max() <= 5e-6 * max(1.0, np.abs(wl).max())
+
+
 # ---- appending -----------------------------------------------------------------------------------
 def _freq(half, base=10000.0):
     return (base ** (-torch.arange(half, dtype=torch.float64) / max(1, half))).float()
