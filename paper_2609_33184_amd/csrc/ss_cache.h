@@ -85,6 +85,7 @@ struct CacheSeenArgs : CacheAttendArgs {
   const uint64_t *tree;   // [num_rows]: bit j: the row sees the request's j-th row's token; null: a chain
   int32_t window;         // tokens up to its own that a row sees of those before the request's rows; 0: all
   int32_t sinks;          // first tokens that it sees as well
+  int32_t direct;         // a worker is a workgroup that attends all of a (request, KV head, block of rows): nothing to join
 };
 
 struct CacheGroupArgs : CacheSeenArgs {};
@@ -97,8 +98,14 @@ struct CacheSplit {
 };
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
 // From how many rows per KV head on the rows of a tree are attended in groups, and how that is split.
-constexpr int kCacheGroupRows = 65;
+// 16 x 32768 tokens with 40 and 64 rows in bf16 450 and 468 us, with waves for themselves 495 and 513; in 8
+// bits 523 and 525, 354 and 371; 96 rows 537 and 707.
+constexpr int cache_group_rows(int fmt) { return fmt == kCacheBf16 ? 33 : 65; }
 CacheSplit cache_group_split(int fmt, int B, int Hkv, int capacity, int M);
+// Whether one workgroup attends all the tiles (of 32 tokens) of each (request, KV head, block of rows), of which there are `wholes`,
+// without a join.  One request, 8 KV heads, 64 rows on 32 heads in bf16: of 4 tiles 14.8 us, split 16.9; of 8 tiles 20.1 and 18.9, of
+// 16 tiles 31.6 and 21.5.  16 requests of one row over 10 tiles 11.5 and 15.5; 8 of 64 rows over 8 tiles 23.6 and 34.3.
+inline bool cache_attend_direct(int64_t tiles, int64_t wholes) { return tiles <= (wholes < 64 ? 4 : 16); }
 inline int cache_row_blocks(int M) { return (M + kCacheRowBlock - 1) / kCacheRowBlock; }
 
 // Launch wrappers; return hipGetLastError() of the launch.

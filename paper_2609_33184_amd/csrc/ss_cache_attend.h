@@ -125,6 +125,14 @@ __device__ __forceinline__ Seen seen_by(const CacheSeenArgs &p, int n, int row0,
   return s;
 }
 
+// What a worker of a call that is not split attends: its (request, KV head, block of rows).
+struct Whole {
+  int b, h, block;
+};
+__device__ __forceinline__ Whole whole_of(const CacheSeenArgs &p, int worker) {
+  const int pair = (int)((uint32_t)worker / (uint32_t)p.B), block = (int)((uint32_t)pair / (uint32_t)p.Hkv);
+  return {worker - pair * p.B, pair - block * p.Hkv, block};
+}
 // x as a value that the compiler has not seen: of the thread's index, so that it
 // does not keep every address of a piece, a tile and a merge in a register of
 // its own all the way.
@@ -186,6 +194,21 @@ __device__ __forceinline__ f32x4_t row_value(const CacheAttendArgs &p, const Row
   return v;
 }
 
+// The rows of a block of a request without tokens, by the workgroup.
+template <typename Args>
+__device__ __forceinline__ void write_empty(const Args &p, int rows, int row0, const Whole &at) {
+  const int first = kBlockOf<Args> * at.block, behind = rows * p.G < first + kBlockOf<Args> ? rows * p.G : first + kBlockOf<Args>;
+  for (int j = threadIdx.x; j < (behind - first) * (kCacheDim / 4); j += kThreads) {
+    const int r = first + j / (kCacheDim / 4), c = j % (kCacheDim / 4), i = (int)((uint32_t)r * p.g_inv >> 16);
+    const int64_t row = (int64_t)row0 + i;
+    if (row < 0 || row >= p.num_rows) continue;
+    const int64_t o = row * p.Hq + at.h * p.G + r - i * p.G;
+    const RowEnd end = row_end(p, o, kNegInf, 0.f);
+    *reinterpret_cast<f32x4_t *>(p.out + o * kCacheDim + 4 * c) = row_value(p, end, o * kCacheDim + 4 * c, f32x4_t{0.f, 0.f, 0.f, 0.f});
+    if (c == 0 && p.lse != nullptr) p.lse[o] = end.lse;
+  }
+}
+
 // Staged V: 16-byte chunk c of row t lies at c ^ swizzle(t), so that neither the
 // rows' stores (whole rows of 16, 2 x 8 or 4 x 4 chunks) nor the transpose reads
 // (8 rows of two chunks, or 4 rows of four) meet in a bank.
@@ -213,8 +236,8 @@ __device__ __forceinline__ void cut3(float p0, float p1, uint32_t &a, uint32_t &
 // 8 where a pair may have that many: 32768 tokens with 4 heads, 128 states a pair,
 // 8.8 us with 8 and 6.3 with 32), else each takes a row of its own.
 // ---------------------------------------------------------------------------
-template <int SPLIT, typename Args>
-__global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_kernel(Args p) {
+template <int SPLIT>
+__global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_kernel(CacheAttendArgs p) {
   constexpr int kHalves = SPLIT > 8 ? SPLIT : 8, kRowsPer = kHalves / SPLIT;
   const int tx = threadIdx.x, lane = tx & 31;
   const int part = (tx >> 5) % SPLIT;
@@ -238,9 +261,8 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   f32x4_t a = {0.f, 0.f, 0.f, 0.f};
   if (q.tiles > 0) {
     const int share = share_of(all * p.Hkv, p.workers);
-    const int block = kSeen<Args> ? r / kBlockOf<Args> : 0, units = q.tiles + p.piece_units;
-    const int start = h * all + before + block * units;
-    const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + units - 1) / (uint32_t)share);
+    const int start = h * all + before;
+    const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + q.units - 1) / (uint32_t)share);
     mine &= w0 != w1;               // else one worker attended all of it
     if (mine) {
       constexpr int kAhead = SPLIT > 8 ? 4 : 8;     // states in flight
@@ -250,7 +272,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
           const int v = w + j * SPLIT <= w1 ? w + j * SPLIT : w1;
-          const int64_t o = (int64_t)(2 * v + (v == w0 ? 1 : 0)) * part_rows(p) + r - block * kBlockOf<Args>;
+          const int64_t o = (int64_t)(2 * v + (v == w0 ? 1 : 0)) * p.M + r;
           ml[j] = *reinterpret_cast<const f32x2_t *>(p.part_ml + 2 * o);
           x[j] = *reinterpret_cast<const f32x4_t *>(p.part_a + o * kCacheDim + 4 * lane);
         }
@@ -296,16 +318,120 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   if (lane == 0 && p.lse != nullptr) p.lse[row] = end.lse;
 }
 
+// The same for rows that see a tree or a window, which may be many more, in blocks: a workgroup goes over the request's own
+// heads and rows, gridDim.y workgroups a request (24 requests of 6 to 384 rows on 8 heads: a workgroup for every eight that there
+// may be 14.6 us, gone over 12.2).
+template <int SPLIT, typename Args>
+__global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_seen_kernel(Args p) {
+  constexpr int kHalves = SPLIT > 8 ? SPLIT : 8, kRowsPer = kHalves / SPLIT;
+  __shared__ __attribute__((aligned(16))) float sa[SPLIT > 1 ? kHalves : 1][kCacheDim];
+  __shared__ float sm[kHalves], sl[kHalves];
+  const int tx = threadIdx.x, lane = tx & 31;
+  const int part = (tx >> 5) % SPLIT;
+  const int b = blockIdx.x;
+  int before = 0, all = 0;
+  for (int j = tx & 63; j < p.B; j += 64) {
+    const int t = request_at(p, j).units;
+    all += t;
+    before += j < b ? t : 0;
+  }
+  const Request q = request_at(p, b);
+  before = lane_of(wave_scan(before), 63);
+  all = lane_of(wave_scan(all), 63);
+  const int share = share_of(all * p.Hkv, p.workers), units = q.tiles + p.piece_units;
+  const int rows = q.rows * p.G;
+  for (int first = blockIdx.y * kRowsPer; first < p.Hkv * rows; first += gridDim.y * kRowsPer) {
+    const int item = first + (tx >> 5) / SPLIT;
+    const int h = (int)((uint32_t)item / (uint32_t)rows), r = item - h * rows;
+    const int i = (int)((uint32_t)r * p.g_inv >> 16), block = r / kBlockOf<Args>;
+    bool mine = h < p.Hkv && q.row0 + i >= 0 && q.row0 + i < p.num_rows;
+    const int64_t row = ((int64_t)q.row0 + i) * p.Hq + h * p.G + r - i * p.G;
+    float m = kNegInf, l = 0.f;
+    f32x4_t a = {0.f, 0.f, 0.f, 0.f};
+    if (q.tiles > 0) {
+      const int start = h * all + before + block * units;
+      const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + units - 1) / (uint32_t)share);
+      mine &= w0 != w1;               // else one worker attended all of it
+      if (mine) {
+        constexpr int kAhead = 4;     // states in flight
+        for (int w = w0 + part; w <= w1; w += kAhead * SPLIT) {
+          f32x2_t ml[kAhead];
+          f32x4_t x[kAhead];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            const int v = w + j * SPLIT <= w1 ? w + j * SPLIT : w1;
+            const int64_t o = (int64_t)(2 * v + (v == w0 ? 1 : 0)) * part_rows(p) + r - block * kBlockOf<Args>;
+            ml[j] = *reinterpret_cast<const f32x2_t *>(p.part_ml + 2 * o);
+            x[j] = *reinterpret_cast<const f32x4_t *>(p.part_a + o * kCacheDim + 4 * lane);
+          }
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            if (w + j * SPLIT > w1) break;
+            const float mn = fmaxf(m, ml[j][0]);
+            const float fa = mn == kNegInf ? 1.f : exp2_fast(m - mn), fb = mn == kNegInf ? 1.f : exp2_fast(ml[j][0] - mn);
+            a = fa * a + fb * x[j];
+            l = fa * l + fb * ml[j][1];
+            m = mn;
+          }
+        }
+      }
+    }
+    if constexpr (SPLIT > 1) {
+      __syncthreads();
+      *reinterpret_cast<f32x4_t *>(&sa[tx >> 5][4 * lane]) = a;
+      if (lane == 0) {
+        sm[tx >> 5] = m;
+        sl[tx >> 5] = l;
+      }
+      __syncthreads();
+      if (part != 0) continue;
+      float top = kNegInf;
+#pragma unroll
+      for (int j = 0; j < SPLIT; ++j) top = fmaxf(top, sm[(tx >> 5) + j]);
+      a = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      l = 0.f;
+#pragma unroll 8
+      for (int j = 0; j < SPLIT; ++j) {
+        const float f = top == kNegInf ? 1.f : exp2_fast(sm[(tx >> 5) + j] - top);
+        l += f * sl[(tx >> 5) + j];
+        a += f * *reinterpret_cast<const f32x4_t *>(&sa[(tx >> 5) + j][4 * lane]);
+      }
+      m = top;
+    }
+    if (!mine) continue;
+    const RowEnd end = row_end(p, row, m, l);
+    const int64_t o = row * kCacheDim + 4 * lane;
+    *reinterpret_cast<f32x4_t *>(p.out + o) = row_value(p, end, o, a);
+    if (lane == 0 && p.lse != nullptr) p.lse[row] = end.lse;
+  }
+}
+
 // Merge what an attention over p left: 32 or 8 half waves a row where a (request, KV head, block of rows) may have that many states.
 template <typename Args>
 hipError_t launch_join(const Args &p, hipStream_t s) {
-  const int64_t pairs = (int64_t)p.B * p.Hkv * ((p.M + kBlockOf<Args> - 1) / kBlockOf<Args>);
-  if (pairs * 32 <= p.workers)
-    hipLaunchKernelGGL((cache_join_kernel<32, Args>), dim3(p.B, p.Hkv * p.M), dim3(1024), 0, s, p);
-  else if (pairs * 8 <= p.workers)
-    hipLaunchKernelGGL((cache_join_kernel<8, Args>), dim3(p.B, p.Hkv * p.M), dim3(kThreads), 0, s, p);
-  else
-    hipLaunchKernelGGL((cache_join_kernel<1, Args>), dim3(p.B, (p.Hkv * p.M + 7) / 8), dim3(kThreads), 0, s, p);
+  if constexpr (kSeen<Args>) {
+    const int64_t pairs = (int64_t)p.B * p.Hkv * ((p.M + kBlockOf<Args> - 1) / kBlockOf<Args>);
+    // more threads than the chip holds at once only wait: one request, 2048 rows of 32 states 22.4 us with 32 half waves each, 9.0 with 8
+    const bool few = (int64_t)p.B * p.Hkv * p.M <= 512;
+    const auto groups = [&](int rows_per) {
+      const int64_t most = ((int64_t)p.Hkv * p.M + rows_per - 1) / rows_per, some = 2048 / p.B;
+      return dim3(p.B, (unsigned)(most < some ? most : some > 1 ? some : 1));
+    };
+    if (pairs * 32 <= p.workers && few)
+      hipLaunchKernelGGL((cache_join_seen_kernel<32, Args>), groups(1), dim3(1024), 0, s, p);
+    else if (pairs * 8 <= p.workers)
+      hipLaunchKernelGGL((cache_join_seen_kernel<8, Args>), groups(1), dim3(kThreads), 0, s, p);
+    else
+      hipLaunchKernelGGL((cache_join_seen_kernel<1, Args>), groups(8), dim3(kThreads), 0, s, p);
+  } else {
+    const int64_t pairs = (int64_t)p.B * p.Hkv;
+    if (pairs * 32 <= p.workers)
+      hipLaunchKernelGGL((cache_join_kernel<32>), dim3(p.B, p.Hkv * p.M), dim3(1024), 0, s, p);
+    else if (pairs * 8 <= p.workers)
+      hipLaunchKernelGGL((cache_join_kernel<8>), dim3(p.B, p.Hkv * p.M), dim3(kThreads), 0, s, p);
+    else
+      hipLaunchKernelGGL((cache_join_kernel<1>), dim3(p.B, (p.Hkv * p.M + 7) / 8), dim3(kThreads), 0, s, p);
+  }
   return hipGetLastError();
 }
 

@@ -148,9 +148,9 @@ struct AttendLayout {
   bool group;         // attended by the kernel of many rows
   ss::CacheSplit split;
   size_t ml, bytes;   // offset of the maxima and sums; all of it
-  explicit AttendLayout(const ss_cache_desc *d) {
+  explicit AttendLayout(const ss_cache_desc *d, bool grouped = false) {      // grouped: many rows may be
     M = d->max_rows * (d->num_q_heads / d->num_kv_heads);
-    group = M >= ss::kCacheGroupRows;
+    group = grouped && M >= ss::cache_group_rows(d->format);
     const int reach = d->table_stride * d->page_tokens, block = group ? ss::kCacheGroupBlock : ss::kCacheRowBlock;
     split = group ? ss::cache_group_split(d->format, d->num_requests, d->num_kv_heads, reach, M)
                   : ss::cache_attend_split(d->format, d->num_requests, d->num_kv_heads, reach, M);
@@ -160,8 +160,21 @@ struct AttendLayout {
   }
 };
 
+// What the rows of a tree or in a window see; calls over few tokens are not split.
+void fill_seen(ss::CacheSeenArgs *p, const ss_cache_desc *d, const AttendLayout &layout, const uint64_t *tree, int32_t window, int32_t sinks) {
+  p->tree = tree;
+  p->window = window;
+  p->sinks = sinks;
+  int64_t reach = p->capacity;
+  // a window's tokens begin and end within a tile, and so do the first ones
+  if (window > 0 && (int64_t)window + sinks + d->max_rows < reach) reach = (int64_t)window + sinks + d->max_rows + 3 * ss::kCacheTile;
+  const int block = layout.group ? ss::kCacheGroupBlock : ss::kCacheRowBlock, wholes = p->B * p->Hkv * ((layout.M + block - 1) / block);
+  p->direct = !layout.split.alone && ss::cache_attend_direct((reach + ss::kCacheTile - 1) / ss::kCacheTile, wholes);
+  if (p->direct) p->workers = wholes;
+}
+
 // The checks and arguments that the attentions share, once the descriptor is checked.
-ss_status prepare_attend(ss::CacheAttendArgs *p, const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const void *q,
+ss_status prepare_attend(ss::CacheAttendArgs *p, const AttendLayout &layout, const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const void *q,
                          int64_t q_row_stride, int32_t num_rows, const int32_t *row_start, const int32_t *end, float *out, float *lse,
                          const float *prev_out, const float *prev_lse, void *workspace, size_t workspace_bytes, hipStream_t stream) {
   const int64_t packed = (int64_t)desc->num_q_heads * ss::kCacheDim;
@@ -174,7 +187,6 @@ ss_status prepare_attend(ss::CacheAttendArgs *p, const ss_cache_desc *desc, cons
     return fail(SS_ERR_INVALID_ARGUMENT, "prev_out and prev_lse come together");
   if (!aligned(prev_out, 16) || !aligned(prev_lse, 4))
     return fail(SS_ERR_INVALID_ARGUMENT, "prev_out must be 16-byte and prev_lse 4-byte aligned");
-  const AttendLayout layout(desc);
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layout.bytes)
     return fail(SS_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold %zu bytes (got %p, %zu)", layout.bytes, workspace,
                 workspace_bytes);
@@ -273,7 +285,7 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
   ss_status s = check_attend_desc(desc);
   if (s != SS_OK) return s;
   ss::CacheAttendArgs p;
-  s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
+  s = prepare_attend(&p, AttendLayout(desc), desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
                      workspace_bytes, stream);
   if (s != SS_OK) return s;
   const hipError_t e = ss::launch_cache_attend(p, desc->format, stream);
@@ -282,7 +294,7 @@ ss_status ss_cache_attend(const ss_cache_desc *desc, const void *pages, const in
 
 size_t ss_cache_attend_tree_workspace_bytes(const ss_cache_desc *desc) {
   if (check_tree_desc(desc) != SS_OK) return 0;
-  return AttendLayout(desc).bytes;
+  return AttendLayout(desc, true).bytes;
 }
 
 ss_status ss_cache_attend_tree(const ss_cache_desc *desc, const void *pages, const int32_t *page_table, const uint64_t *tree,
@@ -294,15 +306,14 @@ ss_status ss_cache_attend_tree(const ss_cache_desc *desc, const void *pages, con
   if (tree == nullptr || !aligned(tree, 8)) return fail(SS_ERR_INVALID_ARGUMENT, "tree must be non-null and 8-byte aligned");
   s = check_window(window, sinks, 0);
   if (s != SS_OK) return s;
+  const AttendLayout layout(desc, true);
   ss::CacheGroupArgs p;
-  s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
+  s = prepare_attend(&p, layout, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
                      workspace_bytes, stream);
   if (s != SS_OK) return s;
-  p.tree = tree;
-  p.window = window;
-  p.sinks = sinks;
-  const hipError_t e = AttendLayout(desc).group ? ss::launch_cache_attend_group(p, desc->format, stream)
-                                                : ss::launch_cache_attend_seen(p, desc->format, stream);
+  fill_seen(&p, desc, layout, tree, window, sinks);
+  const hipError_t e = layout.group ? ss::launch_cache_attend_group(p, desc->format, stream)
+                                    : ss::launch_cache_attend_seen(p, desc->format, stream);
   return e == hipSuccess ? SS_OK : hip_fail(e, "cache tree attention launch");
 }
 
@@ -315,13 +326,12 @@ ss_status ss_cache_attend_window(const ss_cache_desc *desc, const void *pages, c
   if (desc->causal != 1) return fail(SS_ERR_INVALID_ARGUMENT, "a window takes causal = 1");
   s = check_window(window, sinks, 1);
   if (s != SS_OK) return s;
+  const AttendLayout layout(desc);
   ss::CacheSeenArgs p;
-  s = prepare_attend(&p, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
+  s = prepare_attend(&p, layout, desc, pages, page_table, q, q_row_stride, num_rows, row_start, end, out, lse, prev_out, prev_lse, workspace,
                      workspace_bytes, stream);
   if (s != SS_OK) return s;
-  p.tree = nullptr;
-  p.window = window;
-  p.sinks = sinks;
+  fill_seen(&p, desc, layout, nullptr, window, sinks);
   const hipError_t e = ss::launch_cache_attend_seen(p, desc->format, stream);
   return e == hipSuccess ? SS_OK : hip_fail(e, "cache window attention launch");
 }
