@@ -30,6 +30,9 @@ struct Half {      // bounds of a scale byte
   static constexpr uint32_t kLeast = 127 - (FMT == kCacheMx8 ? 23 : 31), kMost = 127 + (FMT == kCacheMx8 ? -1 : 5);
 };
 
+// Scale bytes beyond which V's sums might pass the largest number with these factors: from such a tile on a piece goes without.
+constexpr uint32_t kHuge = 127 + 60;
+
 template <int I>
 using Int = std::integral_constant<int, I>;
 
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   constexpr int kLanes = kRow / 16;                        // lanes of a stored row
   __shared__ __attribute__((aligned(256))) unsigned char smem[kBuffers][2][kTileBytes];     // tiles' K, V
   __shared__ float merge_m[2][64], merge_l[2][64];
-  __shared__ int wide[kBuffers];                           // the tile's number if some of its V is beyond half precision
+  __shared__ int wide[kBuffers], huge[kBuffers];           // the tile's number if some of its V is beyond half precision, or beyond kHuge
   __shared__ int spoilt[kBuffers];                         // its number if some is no number at tokens that not all rows see:
   __shared__ __attribute__((aligned(16))) uint8_t no_number[kBuffers][kTokens][kCacheDim / 8];      // which, a bit each
   __shared__ Request window[kWaves][64];                   // requests base .. base + 63, each wave its own copy: the registers are full
@@ -321,10 +324,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
       for (int j = 0; j < 4; ++j) y[j] = none ? 0u : y[j];
       vs[set] = none ? 127 : vs[set];
     }
-    if (__builtin_amdgcn_ballot_w64(vs[set] - Half<FMT>::kLeast > Half<FMT>::kMost - Half<FMT>::kLeast) != 0) {
+    bool beyond = vs[set] - Half<FMT>::kLeast > Half<FMT>::kMost - Half<FMT>::kLeast;
+    if constexpr (FMT == kCacheMx8) {      // a value that is no number by itself, which the writes make none of
+      uint32_t none = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) none |= (y[j] & 0x7f7f7f7fu) + 0x01010101u;
+      beyond |= (none & 0x80808080u) != 0;
+    }
+    if (__builtin_amdgcn_ballot_w64(beyond) != 0) {
       const uint32_t any = (y[0] | y[1] | y[2] | y[3]) & (FMT == kCacheMx8 ? 0x7f7f7f7fu : 0x77777777u);      // zeros fit with any scale but NaN's
-      const bool beyond = vs[set] - Half<FMT>::kLeast > Half<FMT>::kMost - Half<FMT>::kLeast && (any != 0 || vs[set] == 255);
-      if (beyond) wide[number & (kBuffers - 1)] = number;
+      if (beyond && (any != 0 || vs[set] == 255)) wide[number & (kBuffers - 1)] = number;
+      if (vs[set] > kHuge && any != 0) huge[number & (kBuffers - 1)] = number;
     }
   };
   // In a tile in LDS that some rows see a part of, V's values that are no numbers become zeros: a weight of zero would
@@ -356,7 +366,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   // their way to registers.
   enter();
   if (lp.tiles == 0) return;
-  if (thread < kBuffers) wide[thread] = spoilt[thread] = -1;
+  if (thread < kBuffers) wide[thread] = huge[thread] = spoilt[thread] = -1;
   workgroup_barrier();
   int exacts = kHalf ? 0 : -1;      // bit i % kBuffers: tile i's V is bf16
   auto bring = [&](auto parity, int number) {      // tile `number` from registers into LDS, behind the barrier that follows its tell
@@ -392,7 +402,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   float m_run = kNegInf, l_run = 0.f;
   f32x16_t acc[kAccs], x = f32x16_t{};      // x: the scores of the tile that this wave attends next
   int M = 0, first_row = 0, groups = 1, mine = 0, turn = 0;      // rows of the block; of all, its first; waves per 32 rows; this wave's rows, its tiles
-  bool works = false;
+  bool works = false, plain = false;      // whether it has rows; its state goes without the factors of half precision
   // S^T = K Q^T of a tile: K's rows read, and multiplied.
   auto read_k = [&](int number, int lane, u32x4_t (&kw)[kSteps]) {
     // chunk 2 s + lq of row lr, at (2 s + lq) ^ (lr & 15): s flips bits of the first one's place
@@ -452,6 +462,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
       low = seen.low;
       m_run = kNegInf;
       l_run = 0.f;
+      plain = false;
 #pragma unroll
       for (int a = 0; a < kAccs; ++a) acc[a] = f32x16_t{};
     }
@@ -513,10 +524,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
         for (int a = 0; a < kAccs; ++a) acc[a] *= alpha;
         m_run = mn;
       }
-      const float ms = m_run == kNegInf ? 0.f : kHalf ? m_run - kPShift : m_run;
-
       if (kHalf && __builtin_expect(exact, 0)) {
+        if (!plain && one(huge[buf]) == number) {
+          plain = true;
+          l_run *= 1.f / (1 << kPShift);
+#pragma unroll
+          for (int a = 0; a < kAccs; ++a) acc[a] *= 1.f / (1 << (kPShift + kVShift));
+        }
+      }
+      const float ms = m_run == kNegInf ? 0.f : kHalf && !plain ? m_run - kPShift : m_run;
+
+      if (kHalf && __builtin_expect(exact || plain, 0)) {
         // V beyond half precision, which may be no number: each token is added to the rows that see it
+        const float factor = exact ? plain ? 1.f : (float)(1 << kVShift) : 1.f / (1 << kVShift);
 #pragma unroll 1
         for (int t = 0; t < 32; ++t) {
           const int e = 4 * (t >> 3) + (t & 3);
@@ -531,8 +551,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
           for (int c = 0; c < 16; ++c) {
             const u32x2_t y = *reinterpret_cast<const u32x2_t *>(smem[buf][1] + t * 256 + 16 * (c ^ swizzle<FMT, 32>(t)) + 8 * lq);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              acc[c >> 2][4 * (c & 3) + j] += pe * (float)(1 << kVShift) * __uint_as_float(j & 1 ? y[j >> 1] & 0xffff0000u : y[j >> 1] << 16);
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t v = j & 1 ? y[j >> 1] >> 16 : y[j >> 1] & 0xffffu;
+              acc[c >> 2][4 * (c & 3) + j] += pe * factor * (exact ? __uint_as_float(v << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)v));
+            }
           }
         }
         u32x4_t kw[kSteps];
@@ -621,10 +643,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
 
     if (k + 1 == tiles) {      // the piece ends: its states, or its result
       const int lane = hidden(thread & 63), lr = lane & 31, lq = lane >> 5;
-      float m = kHalf ? m_run - kPShift : m_run, l = xgroup_sum<2>(l_run);
+      float m = kHalf && !plain ? m_run - kPShift : m_run, l = xgroup_sum<2>(l_run);
 #pragma unroll
       for (int a = 0; a < kAccs; ++a)
-        if constexpr (kHalf) acc[a] *= 1.f / (1 << kVShift);
+        if constexpr (kHalf) acc[a] *= plain ? 1.f : 1.f / (1 << kVShift);
       auto piece_of = [&](int c) {
         return f32x4_t{acc[c >> 2][4 * (c & 3)], acc[c >> 2][4 * (c & 3) + 1], acc[c >> 2][4 * (c & 3) + 2], acc[c >> 2][4 * (c & 3) + 3]};
       };

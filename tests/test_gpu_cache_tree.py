@@ -386,6 +386,56 @@ def test_tree_values_of_every_size(fmt, hq, n, factor):
     assert np.abs(r.lse.cpu().numpy() - wl).max() <= 5e-6 * max(1.0, np.abs(wl).max())
 
 
+@pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
+@pytest.mark.parametrize("hq,n", ((8, 7), (8, 40), (16, 64)))
+@pytest.mark.parametrize("where", ("history", "tree", "all"))
+def test_tree_values_near_the_largest(fmt, hq, n, where):
+    """Values of up to 2^114 in one block of 32 channels: each block is as near as if it were alone.
+
+    The scores are normal numbers: exp of 500 of them adds up to less than 2^10, and the running maximum is above 2^-1. No
+    sum that the formula needs passes 2^114 * 2^11, so any overflow is the kernel's own.
+    """
+    rng = np.random.default_rng(n)
+    end = [400 + n, 70 + n]
+    v = _normal(6, sum(end), 2, 128)
+    which = {"history": slice(100, 133), "tree": slice(end[0] - 3, end[0]), "all": slice(0, sum(end))}[where]
+    v[which, :, 32:64] *= 2.0 ** 112
+    c = Cache(fmt, 2, 32, end)
+    c.fill_tokens(end, 5, v=v)
+    r = TreeRows(c, hq, _trees(rng, (n, n)), end).run()
+    torch.cuda.synchronize()
+    want, wl = r.want()
+    got = r.out.cpu().numpy().astype(np.float64)
+    assert np.isfinite(got).all()
+    for b in range(4):
+        g, x = got[..., 32 * b:32 * b + 32], want[..., 32 * b:32 * b + 32]
+        for mine in (slice(0, n), slice(n, 2 * n)):
+            assert np.linalg.norm(g[mine] - x[mine]) <= 5e-6 * np.linalg.norm(x[mine])
+    assert np.abs(r.lse.cpu().numpy() - wl).max() <= 5e-6 * max(1.0, np.abs(wl).max())
+
+
+@pytest.mark.parametrize("hq,n", ((4, 7), (8, 40), (8, 64)))
+def test_tree_codes_that_are_no_numbers(hq, n):
+    """An e4m3 code that is none, under an ordinary scale, in a node's V: rows that do not see it stay as they are."""
+    rng = np.random.default_rng(n)
+    end, words = [64 + n], _trees(rng, (n,))
+    node = n // 2
+    t = 64 + node
+    c = Cache(oc.MXFP8, 1, 32, end)
+    c.fill_tokens(end, 5)
+    oc.parts(c.pages, oc.MXFP8, 32)[1][c.table[0, t // 32], 0, t % 32, 77] = 0x7F
+    c.dev.copy_(torch.from_numpy(c.pages))
+    r = TreeRows(c, hq, words, end).run()
+    torch.cuda.synchronize()
+    want, _ = r.want()
+    got = r.out.cpu().numpy()
+    for i in range(n):
+        if words[0][i] >> node & 1:
+            assert np.isnan(got[i, :, 77]).all() and np.isnan(want[i, :, 77]).all()
+            got[i, :, 77] = want[i, :, 77] = 0
+    assert np.abs(got - want).max() <= r._bound()
+
+
 # ---- appending -----------------------------------------------------------------------------------
 def _freq(half, base=10000.0):
     return (base ** (-torch.arange(half, dtype=torch.float64) / max(1, half))).float()
