@@ -484,10 +484,10 @@ typedef struct {
 } ss_rope_desc;
 
 /* Write rows into the cache, K turned: as ss_cache_write does with the turned rows
- * rounded to bf16, bit for bit, in every format (a turned value is off by its
- * rounding and 2^-22 of the pair's length at most).  positions: null (a row's
- * position is its token's, end[b] - n_b + i) or device int32 [num_rows], of any
- * sign (a history that lies elsewhere, a tree).  q, q_out: both null, or device
+ * rounded to bf16, bit for bit, in every format (a turned value is worked out in
+ * 64 bits, off by 2^-34 of the pair's length at most, and rounded to fp32 and then
+ * to bf16).  positions: null (a row's position is its token's, end[b] - n_b + i) or
+ * device int32 [num_rows], of any sign (a history that lies elsewhere, a tree).  q, q_out: both null, or device
  * bf16 rows r at element r * q_row_stride (q_out_row_stride; 0: packed, Hq * d) that
  * are turned alike (num_q_heads matters then); q_out may be q with the same
  * stride and must not overlap it otherwise, nor k and v.  A row whose token has no

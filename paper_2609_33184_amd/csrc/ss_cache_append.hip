@@ -18,25 +18,32 @@ namespace {
 // sines are computed once.  Pairs half a rotated head apart lie in lanes half of
 // its lanes apart and are exchanged, neighbouring pairs lie in a lane.
 //
-// Precision.  The angle in turns is a product of 64 bits, of which the whole
-// quarters are taken off before it enters 32: a position of 2^31 costs 2^-25 turns.
-// Sine and cosine are Taylor series over an eighth of a turn either way, off by 2e-9
-// beside their fp32 roundings.  A turned channel is rounded to bf16 once; K is
-// quantised from there, so that a cache is bit for bit the one that the rotated
-// rows' ss_cache_write gives.
+// Precision.  All of it is in 64 bits, whose products cost what those of 32 do here:
+// the angle, which grows with the position; its rest of a quarter turn, taken off in
+// two steps; sine and cosine, Taylor series over an eighth of a turn either way, off
+// by 7e-12; the turned pair.  That is rounded to fp32 and then to bf16, as a
+// reference in 64 bits rounds it; K is quantised from there, so that a cache is bit
+// for bit the one that the rotated rows' ss_cache_write gives.
 // ---------------------------------------------------------------------------
 
-// cos and sin of p f.  1/362880 etc.: the series' coefficients.
-__device__ __forceinline__ void turn_of(double p, float f, float scale, float &c, float &s) {
-  const double quarters = p * (double)f * 0.63661977236758134;      // 2 / pi
-  const double whole = __builtin_rint(quarters);
-  const float x = (float)(quarters - whole) * 1.5707963267948966f, y = x * x;
-  const int q = (int)(whole - 4.0 * __builtin_floor(whole * 0.25));
-  const float sx = __builtin_fmaf(x * y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), x);
-  const float cx = __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
-  const float a = q & 1 ? sx : cx, b = q & 1 ? cx : sx;
-  c = scale * ((q + 1) & 2 ? -a : a);
-  s = scale * (q & 2 ? -b : b);
+// cos and sin of p f.
+__device__ __forceinline__ void turn_of(double p, float f, double scale, double &c, double &s) {
+  const double a = p * (double)f, n = __builtin_rint(a * 0.63661977236758134);                            // 2 / pi
+  const double x = __builtin_fma(-n, 6.123233995736766e-17, __builtin_fma(-n, 1.5707963267948966, a));      // pi / 2 in two parts
+  const double y = x * x;
+  const int q = (int)(n - 4.0 * __builtin_floor(n * 0.25));
+  double u = __builtin_fma(y, -1.0 / 39916800, 1.0 / 362880), v = __builtin_fma(y, 1.0 / 479001600, -1.0 / 3628800);
+  u = __builtin_fma(y, u, -1.0 / 5040);
+  u = __builtin_fma(y, u, 1.0 / 120);
+  u = __builtin_fma(y, u, -1.0 / 6);
+  v = __builtin_fma(y, v, 1.0 / 40320);
+  v = __builtin_fma(y, v, -1.0 / 720);
+  v = __builtin_fma(y, v, 1.0 / 24);
+  v = __builtin_fma(y, v, -0.5);
+  const double sx = __builtin_fma(x * y, u, x), cx = __builtin_fma(y, v, 1.0);
+  const double k = q & 1 ? sx : cx, l = q & 1 ? cx : sx;
+  c = scale * ((q + 1) & 2 ? -k : k);
+  s = scale * (q & 2 ? -l : l);
 }
 
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
@@ -45,8 +52,21 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)lo, (__bf16)hi});
 }
 
+__device__ __forceinline__ double from_lane(double x, int lane) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)w), hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)(w >> 32));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// To fp32 and no further: the compiler would join this rounding and that to bf16, which costs nine instructions more.
+__device__ __forceinline__ float rounded(double x) {
+  float y = (float)x;
+  asm("" : "+v"(y));
+  return y;
+}
+
 struct Turn {
-  float c[8], s[8];      // of the lane's channels: y = c x + s partner; of neighbouring pairs the even ones count
+  double c[8], s[8];     // of the lane's channels: y = c x + s partner; of its neighbouring pairs: the first four
   int partner;           // the lane that holds the partners; itself: neighbouring pairs
   bool turns;            // whether the lane's channels turn at all
 };
@@ -56,16 +76,18 @@ __device__ __forceinline__ Turn turn_at(const CacheAppendArgs &p, int64_t pos, i
   r.turns = 8 * c < p.rotary_dim;
   const int me = threadIdx.x & 63;
   r.partner = p.interleaved || !r.turns ? me : c < lanes ? me + lanes : me - lanes;
+  // A lane's four neighbouring pairs, or half of the eight that it has with its partner, who brings the others.
+  const bool lower = c < lanes;
+  const int first = p.interleaved ? 4 * c : lower ? 8 * c : 8 * (c - lanes) + 4;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (p.interleaved && (j & 1)) {
-      r.c[j] = r.s[j] = 0.f;
-      continue;
-    }
-    const int channel = 8 * c + j;
-    const int at = !r.turns ? 0 : p.interleaved ? channel / 2 : channel < half ? channel : channel - half;
-    turn_of((double)pos, p.inv_freq[at], p.scale, r.c[j], r.s[j]);
-    if (!p.interleaved && channel < half) r.s[j] = -r.s[j];
+  for (int j = 0; j < 4; ++j) {
+    double cj, sj;
+    turn_of((double)pos, p.inv_freq[r.turns ? first + j : 0], p.scale, cj, sj);
+    const double co = from_lane(cj, r.partner), so = from_lane(sj, r.partner);
+    r.c[j] = p.interleaved || lower ? cj : co;
+    r.s[j] = p.interleaved ? sj : lower ? -sj : so;
+    r.c[4 + j] = lower ? co : cj;
+    r.s[4 + j] = lower ? -so : sj;
   }
   return r;
 }
@@ -74,15 +96,15 @@ __device__ __forceinline__ u32x4_t turned(const CacheAppendArgs &p, const Turn &
   if (p.interleaved) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float a = low_of(x[j]), b = high_of(x[j]), c = r.c[2 * j], s = r.s[2 * j];
-      y[j] = pack_bf16(__builtin_fmaf(a, c, -(b * s)), __builtin_fmaf(b, c, a * s));
+      const double a = low_of(x[j]), b = high_of(x[j]), c = r.c[j], s = r.s[j];
+      y[j] = pack_bf16(rounded(__builtin_fma(a, c, -(b * s))), rounded(__builtin_fma(b, c, a * s)));
     }
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t o = (uint32_t)__shfl((int)x[j], r.partner);
-      y[j] = pack_bf16(__builtin_fmaf(low_of(x[j]), r.c[2 * j], low_of(o) * r.s[2 * j]),
-                       __builtin_fmaf(high_of(x[j]), r.c[2 * j + 1], high_of(o) * r.s[2 * j + 1]));
+      y[j] = pack_bf16(rounded(__builtin_fma((double)low_of(x[j]), r.c[2 * j], (double)low_of(o) * r.s[2 * j])),
+                       rounded(__builtin_fma((double)high_of(x[j]), r.c[2 * j + 1], (double)high_of(o) * r.s[2 * j + 1])));
     }
   }
   return r.turns ? y : x;

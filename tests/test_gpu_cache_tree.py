@@ -3,9 +3,9 @@
 Attention: the same sums as plain attention over fewer tokens, so the same tolerances (5e-6 in the 2-norm, and the
 worst case of a value, ``Rows._bound``; see test_gpu_cache).
 
-Turning.  A sine or cosine is off by the reduced angle's rounding (2^-25 of a quarter turn: below 2^-24), the series
-(2e-9) and its five roundings of at most 2^-24 in sum; two products and a sum add 3 x 2^-24 relative to the pair's
-length.  Together less than 2^-21 of the pair's length; then one rounding to bf16, half a step: 2^-8 of the value.  K
+Turning.  The angle is the product of 64 bits that the oracle takes; the series are off by 7e-12, below 2^-37, and a
+handful of roundings of 2^-53 follow: together less than 2^-34 of the pair's length.  A number that near the oracle's is
+rounded to fp32 and then to bf16, so the result lies between the roundings of the oracle's value less and more 2^-34.  K
 is stored from the bf16 value by exact rules, so a cache is compared byte for byte with the write of the turned rows
 that the GPU returned as Q.
 """
@@ -462,14 +462,18 @@ def _append(c, hq, rows, end, rotary, interleaved, positions=None, scale=1.0, se
     return before, out, start, pos, freq.cpu().numpy()
 
 
-def _close(got_bits, want, rotary, interleaved, scale=1.0):
-    """Half a step of bf16 and 2^-21 of the pair's length; channels that do not turn are equal."""
+def _close(got_bits, want, rotary, interleaved):
+    """Between the roundings of what is 2^-34 of the pair's length off either way; channels that do not turn are equal."""
+    def rounded(x):
+        bits = x.astype(np.float32).view(np.uint32)
+        return bf16_bits_to_f64(((bits + 0x7fff + (bits >> 16 & 1)) >> 16).astype(np.uint16))
     got = bf16_bits_to_f64(got_bits)
     half = rotary // 2
     a, b = (np.arange(0, rotary, 2), np.arange(1, rotary, 2)) if interleaved else (np.arange(half), np.arange(half, rotary))
     length = np.zeros(want.shape)
     length[..., a] = length[..., b] = np.hypot(want[..., a], want[..., b])
-    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -21 * length + 2.0 ** -133).all()
+    off = 2.0 ** -34 * length + 2.0 ** -134
+    assert (rounded(want - off) <= got).all() and (got <= rounded(want + off)).all()
     assert np.array_equal(got[..., rotary:], want[..., rotary:])
 
 
@@ -523,14 +527,7 @@ def test_append_far_positions(interleaved):
     positions = np.array([0, 1, -1, 2147483647, -2147483648, 1 << 30, 1000003, 131071] + [777] * 24 + list(range(1 << 20, (1 << 20) + 32)), np.int64)
     c = Cache(oc.BF16, 2, 32, end)
     (q, k, v), out, start, pos, freq = _append(c, 8, rows, end, 128, interleaved, positions=positions, scale=1.25)
-    # at 2^31 the turns are off by 2^-25 of a quarter... and 2^31 x 2^-53 quarters: below 2^-22 of the length
-    want = ot.turned(q, pos, freq, interleaved, 1.25)
-    got = bf16_bits_to_f64(_bits(out))
-    half = np.arange(64)
-    a, b = (2 * half, 2 * half + 1) if interleaved else (half, half + 64)
-    length = np.zeros(want.shape)
-    length[..., a] = length[..., b] = np.hypot(want[..., a], want[..., b])
-    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -20 * length).all()
+    _close(_bits(out), ot.turned(q, pos, freq, interleaved, 1.25), 128, interleaved)
 
 
 def test_append_places_rows_and_leaves_the_rest():
