@@ -85,7 +85,7 @@ struct CacheSeenArgs : CacheAttendArgs {
   const uint64_t *tree;   // [num_rows]: bit j: the row sees the request's j-th row's token; null: a chain
   int32_t window;         // tokens up to its own that a row sees of those before the request's rows; 0: all
   int32_t sinks;          // first tokens that it sees as well
-  int32_t direct;         // a worker is a workgroup that attends all of a (request, KV head, block of rows): nothing to join
+  int32_t parts;          // a worker has one of as many parts of a (request, KV head, block of rows); 0: shares of all the units
 };
 
 struct CacheGroupArgs : CacheSeenArgs {};
@@ -102,10 +102,22 @@ CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
 // bits 523 and 525, 354 and 371; 96 rows 537 and 707.
 constexpr int cache_group_rows(int fmt) { return fmt == kCacheBf16 ? 33 : 65; }
 CacheSplit cache_group_split(int fmt, int B, int Hkv, int capacity, int M);
-// Whether one workgroup attends all the tiles (of 32 tokens) of each (request, KV head, block of rows), of which there are `wholes`,
-// without a join.  One request, 8 KV heads, 64 rows on 32 heads in bf16: of 4 tiles 14.8 us, split 16.9; of 8 tiles 20.1 and 18.9, of
+// Into how many parts of as many tiles (of 32 tokens) each of `wholes` (request, KV head, block of rows) is cut, a workgroup to a
+// part, with at most `most` workgroups; 1: nothing to join; 0: cut by the lengths, into equal shares of all the units.
+// Few tiles are not cut.  One request, 8 KV heads, 64 rows on 32 heads in bf16: 4 tiles 14.8 us, cut 16.9; 8 tiles 20.1 and 18.9;
 // 16 tiles 31.6 and 21.5.  16 requests of one row over 10 tiles 11.5 and 15.5; 8 of 64 rows over 8 tiles 23.6 and 34.3.
-inline bool cache_attend_direct(int64_t tiles, int64_t wholes) { return tiles <= (wholes < 64 ? 4 : 16); }
+// Where a window makes the lengths alike, equal parts are as even as equal shares and none straddles two requests: 16 requests of 8
+// rows, 64 per KV head, in a window of 1024 29.3 us, shares 34.4; 64 requests of one row in a window of 4096 in bf16 162 and 171;
+// trees of 32 rows, 128 per KV head, in one of 4096 94.9 and 101.4.
+// Not where a part would be long: a single full window among short requests takes as long as its part, 50 us for 129 tiles.
+inline int cache_attend_parts(int64_t tiles, int64_t wholes, int64_t most, bool alike) {
+  if (tiles <= (wholes < 64 ? 4 : 16)) return 1;
+  if (!alike) return 0;
+  int64_t parts = most / wholes;
+  parts = parts > tiles / 4 ? tiles / 4 : parts;
+  parts = parts < 1 ? 1 : parts;
+  return (tiles + parts - 1) / parts <= 160 ? (int)parts : 0;
+}
 inline int cache_row_blocks(int M) { return (M + kCacheRowBlock - 1) / kCacheRowBlock; }
 
 // Launch wrappers; return hipGetLastError() of the launch.

@@ -249,19 +249,18 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   // requests are counted 64 at a time, lane j keeping the units of chunk j.
   Request win;            // requests base .. base + 63
   int base = 0, idx, skip, h, left;   // the next request, its units that are not ours, its head; our units
-  bool direct = false;
-  if constexpr (kSeen<Args>) direct = p.direct != 0;
-  if (direct) {
+  bool even = false;
+  if constexpr (kSeen<Args>) even = p.parts > 0;
+  if (even) {
     if constexpr (kSeen<Args>) {
       const Whole at = whole_of(p, worker);
       base = at.b & ~63;
       idx = at.b & 63;
       h = at.h;
       win = request_at(p, base + (thread & 63));
-      left = lane_of(win.tiles, idx) + p.piece_units;
-      skip = at.block * left;
-      if (lane_of(win.tiles, idx) == 0) write_empty(p, lane_of(win.rows, idx), lane_of(win.row0, idx), at);
-      if (skip >= lane_of(win.units, idx)) return;      // without tokens, or fewer rows
+      at.units(p, lane_of(win.tiles, idx), skip, left);
+      if (lane_of(win.tiles, idx) == 0 && p.parts == 1) write_empty(p, lane_of(win.rows, idx), lane_of(win.row0, idx), at);
+      if (left == 0 || skip >= lane_of(win.units, idx)) return;      // without tokens, or fewer rows
     }
   } else {
     const int lane = thread & 63;
@@ -837,7 +836,7 @@ hipError_t attend(const Args &p, hipStream_t s) {
   }
   const hipError_t e = hipGetLastError();
   if constexpr (kSeen<Args>) {
-    if (p.direct) return e;
+    if (p.parts == 1) return e;
   }
   return e == hipSuccess ? launch_join(p, s) : e;
 }

@@ -125,13 +125,21 @@ __device__ __forceinline__ Seen seen_by(const CacheSeenArgs &p, int n, int row0,
   return s;
 }
 
-// What a worker of a call that is not split attends: its (request, KV head, block of rows).
+// What a worker of a call that is cut into parts attends: part `part` of its (request, KV head, block of rows).
 struct Whole {
-  int b, h, block;
+  int b, h, block, part;
+  // of the request's units: the first one, and how many (none where no tile is left)
+  __device__ __forceinline__ void units(const CacheSeenArgs &p, int tiles, int &skip, int &left) const {
+    const int each = (int)((uint32_t)(tiles + p.parts - 1) / (uint32_t)p.parts), from = part * each;
+    const int there = tiles - from < each ? tiles - from : each;
+    skip = block * (tiles + p.piece_units) + (part == 0 ? 0 : p.piece_units + from);
+    left = there <= 0 ? 0 : there + (part == 0 ? p.piece_units : 0);
+  }
 };
 __device__ __forceinline__ Whole whole_of(const CacheSeenArgs &p, int worker) {
-  const int pair = (int)((uint32_t)worker / (uint32_t)p.B), block = (int)((uint32_t)pair / (uint32_t)p.Hkv);
-  return {worker - pair * p.B, pair - block * p.Hkv, block};
+  const int whole = (int)((uint32_t)worker / (uint32_t)p.parts);
+  const int pair = (int)((uint32_t)whole / (uint32_t)p.B), block = (int)((uint32_t)pair / (uint32_t)p.Hkv);
+  return {whole - pair * p.B, pair - block * p.Hkv, block, worker - whole * p.parts};
 }
 // x as a value that the compiler has not seen: of the thread's index, so that it
 // does not keep every address of a piece, a tile and a merge in a register of
@@ -330,7 +338,7 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
   const int part = (tx >> 5) % SPLIT;
   const int b = blockIdx.x;
   int before = 0, all = 0;
-  for (int j = tx & 63; j < p.B; j += 64) {
+  for (int j = p.parts > 0 ? p.B : tx & 63; j < p.B; j += 64) {
     const int t = request_at(p, j).units;
     all += t;
     before += j < b ? t : 0;
@@ -349,8 +357,16 @@ __global__ __launch_bounds__(SPLIT > 8 ? 32 * SPLIT : kThreads) void cache_join_
     float m = kNegInf, l = 0.f;
     f32x4_t a = {0.f, 0.f, 0.f, 0.f};
     if (q.tiles > 0) {
-      const int start = h * all + before + block * units;
-      const int w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share), w1 = (int)((uint32_t)(start + units - 1) / (uint32_t)share);
+      int w0, w1;
+      if (p.parts > 0) {
+        const int each = (int)((uint32_t)(q.tiles + p.parts - 1) / (uint32_t)p.parts);
+        w0 = ((block * p.Hkv + h) * p.B + b) * p.parts;
+        w1 = w0 + (int)((uint32_t)(q.tiles - 1) / (uint32_t)each);
+      } else {
+        const int start = h * all + before + block * units;
+        w0 = (int)((uint32_t)(start + p.piece_units) / (uint32_t)share);
+        w1 = (int)((uint32_t)(start + units - 1) / (uint32_t)share);
+      }
       mine &= w0 != w1;               // else one worker attended all of it
       if (mine) {
         constexpr int kAhead = 4;     // states in flight

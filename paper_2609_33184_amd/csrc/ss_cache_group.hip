@@ -98,16 +98,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
 
   // This worker's share and where it starts, as in cache_attend_kernel.
   int base = 0, idx, skip, h, left;
-  if (p.direct) {
+  if (p.parts > 0) {
     const Whole at = whole_of(p, worker);
     base = at.b & ~63;
     idx = at.b & 63;
     h = at.h;
     const Request win = request_at(p, base + (thread & 63));
-    left = lane_of(win.tiles, idx) + p.piece_units;
-    skip = at.block * left;
-    if (lane_of(win.tiles, idx) == 0) write_empty(p, lane_of(win.rows, idx), lane_of(win.row0, idx), at);
-    if (skip >= lane_of(win.units, idx)) return;      // without tokens, or fewer rows
+    at.units(p, lane_of(win.tiles, idx), skip, left);
+    if (lane_of(win.tiles, idx) == 0 && p.parts == 1) write_empty(p, lane_of(win.rows, idx), lane_of(win.row0, idx), at);
+    if (left == 0 || skip >= lane_of(win.units, idx)) return;      // without tokens, or fewer rows
     window[w][thread & 63] = win;
   } else {
     Request win;
@@ -710,7 +709,7 @@ template <int FMT>
 hipError_t attend_group(const CacheGroupArgs &p, hipStream_t s) {
   hipLaunchKernelGGL((cache_attend_group_kernel<FMT>), dim3(p.workers), dim3(kThreads), 0, s, p);
   const hipError_t e = hipGetLastError();
-  return e == hipSuccess && !p.direct ? launch_join(p, s) : e;
+  return e == hipSuccess && p.parts != 1 ? launch_join(p, s) : e;
 }
 
 }  // namespace

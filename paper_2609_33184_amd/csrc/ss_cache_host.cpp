@@ -160,7 +160,7 @@ struct AttendLayout {
   }
 };
 
-// What the rows of a tree or in a window see; calls over few tokens are not split.
+// What the rows of a tree or in a window see, and whether the call is cut into parts.
 void fill_seen(ss::CacheSeenArgs *p, const ss_cache_desc *d, const AttendLayout &layout, const uint64_t *tree, int32_t window, int32_t sinks) {
   p->tree = tree;
   p->window = window;
@@ -169,8 +169,11 @@ void fill_seen(ss::CacheSeenArgs *p, const ss_cache_desc *d, const AttendLayout 
   // a window's tokens begin and end within a tile, and so do the first ones
   if (window > 0 && (int64_t)window + sinks + d->max_rows < reach) reach = (int64_t)window + sinks + d->max_rows + 3 * ss::kCacheTile;
   const int block = layout.group ? ss::kCacheGroupBlock : ss::kCacheRowBlock, wholes = p->B * p->Hkv * ((layout.M + block - 1) / block);
-  p->direct = !layout.split.alone && ss::cache_attend_direct((reach + ss::kCacheTile - 1) / ss::kCacheTile, wholes);
-  if (p->direct) p->workers = wholes;
+  // two workgroups a CU for groups (16 trees of 32 rows in a window of 4096 93 us, one 131), else one (32 requests of one row in a
+  // window of 1024 29.5, two 31.0)
+  const int fill = layout.group ? 512 : 256, most = p->workers < fill ? p->workers : fill;
+  p->parts = layout.split.alone ? 0 : ss::cache_attend_parts((reach + ss::kCacheTile - 1) / ss::kCacheTile, wholes, most, reach < p->capacity);
+  if (p->parts > 0) p->workers = wholes * p->parts;
 }
 
 // The checks and arguments that the attentions share, once the descriptor is checked.

@@ -114,6 +114,32 @@ def test_window_requests_by_the_hundred(fmt):
     WindowRows(c, 16, rng.integers(0, 4, B), end, 70, 5).run().check()
 
 
+@pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
+@pytest.mark.parametrize("hkv,window", ((1, 700), (2, 1500), (16, 600), (48, 700)))
+@pytest.mark.parametrize("tree", (0, 1))
+def test_window_parts(fmt, hkv, window, tree):
+    """A window among short requests: a request's tiles in many parts, fewer tiles than parts, one, none; joined in place."""
+    rng = np.random.default_rng(window + hkv)
+    end = [3000, 0, 5, 1400, 70, 33, 1]
+    rows = [4, 3, 2, 1, 0, 4, 1]
+    if tree:
+        rows = [24, 5, 9, 40, 0, 33, 1] if hkv < 16 else [6, 5, 3, 2, 0, 6, 1]
+    c = Cache(fmt, hkv, 32, end)
+    c.fill_tokens(end, 3)
+    T, hq = sum(rows), 4 * hkv
+    prev = (torch.randn(T, hq, 128, generator=torch.Generator().manual_seed(1)).cuda(), torch.randn(T, hq, generator=torch.Generator().manual_seed(2)).cuda())
+    prev[1][::5] = float("-inf")
+    r = TreeRows(c, hq, _trees(rng, rows), end, window, 40, prev=prev) if tree else WindowRows(c, hq, rows, end, window, 40, prev=prev)
+    r.run().check()
+    first = r.out.clone()
+    r.out.copy_(prev[0])
+    r.lse.copy_(prev[1])
+    r.prev = (r.out, r.lse)
+    r.run()
+    torch.cuda.synchronize()
+    assert torch.equal(first, r.out)
+
+
 def test_window_of_everything_equals_plain_attention():
     """No token is hidden and none skipped: the same tiles in the same shares give the same bits."""
     end, rows = [700, 33, 0, 64], [3, 1, 2, 4]
