@@ -74,11 +74,10 @@ struct CacheAttendArgs : CacheArgs {
   float scale_log2;                     // softmax_scale * log2(e)
 };
 
-// Rows of one KV head that a piece of the attention below holds at most: more are
-// attended in blocks of as many.
-constexpr int kCacheRowBlock = 64;
-// And of the attention of many rows, with the tokens of its tiles.
+// Rows of one KV head that a piece of the attention of many rows holds at most (more are attended in blocks of as many), and
+// the tokens of its tiles.
 constexpr int kCacheGroupBlock = 128, kCacheGroupTile = 32;
+constexpr int kCacheMaxRows = 64;      // rows per KV head of the other attentions
 
 // Rows that see a tree, or a window and the first tokens, instead of a chain.
 struct CacheSeenArgs : CacheAttendArgs {
@@ -118,7 +117,6 @@ inline int cache_attend_parts(int64_t tiles, int64_t wholes, int64_t most, bool 
   parts = parts < 1 ? 1 : parts;
   return (tiles + parts - 1) / parts <= 160 ? (int)parts : 0;
 }
-inline int cache_row_blocks(int M) { return (M + kCacheRowBlock - 1) / kCacheRowBlock; }
 
 // Launch wrappers; return hipGetLastError() of the launch.
 hipError_t launch_cache_write(const CacheRowsArgs &p, int fmt, hipStream_t s);

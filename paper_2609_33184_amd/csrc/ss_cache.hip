@@ -174,6 +174,16 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
 // 1e-7 to 7e-7); sums and accumulators are fp32.  The running maximum moves only
 // where a score passes it by more than 2^8, which keeps a cross-lane maximum
 // and the rescaling out of most tiles; weights up to 2^8 cost no precision.
+//
+// SeenArgs: rows that see a tree, or a window and the first tokens.  Of a request's
+// tiles only those are counted and read of which some row may see a token: the
+// sinks' and, behind the gap, the windows' (Sight); a tile that all rows see whole
+// needs no mask, of the others a word of 32 bits says which tokens a row sees.
+// Where a window makes the lengths alike the call is cut into equal parts of each
+// request instead of equal shares (cache_attend_parts).  64 requests of one row in a
+// window of 4096 in bf16 (1.03 GB) 162 us, 6.3 TB/s; 16 requests of 8 rows, 64 per KV
+// head, in a window of 1024 in 4 bits 26.0 us and 5.1 for the join, of which the
+// SIMDs issue half and the rest is the latency of the first loads and of the merge.
 // ---------------------------------------------------------------------------
 constexpr int kLdsRow = 256;                        // a staged V row, bf16
 constexpr int kVTile = kCacheTile * kLdsRow;
@@ -313,7 +323,6 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     int h, t0, tiles;
     int count;     // this wave's tiles: t0 + ws, + STREAMS, ...
     int ids;       // lane j: page of half tile j of them, -1 for what is none
-    int block;     // of its rows (SeenArgs)
     Sight sight;
   };
   // The request's tile that is the t-th attended one.
@@ -332,13 +341,13 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   };
   auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   auto uniform = [&](const Piece &q) {     // the wave's, in scalar registers
-    return Piece{one(q.b), one(q.rows), one(q.row0), one(q.end), one(q.len), one(q.whole), one(q.h), one(q.t0), one(q.tiles), one(q.count), q.ids, one(q.block),
+    return Piece{one(q.b), one(q.rows), one(q.row0), one(q.end), one(q.len), one(q.whole), one(q.h), one(q.t0), one(q.tiles), one(q.count), q.ids,
                  {one(q.sight.sinks), one(q.sight.gap)}};
   };
   // The share's next piece.  Its units are the piece's cost, then the tiles: a
   // share that ends within the cost leaves the tiles to the next one.
   auto next_piece = [&]() {
-    Piece q = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1, 0, {0, 0}};
+    Piece q = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1, {0, 0}};
     while (left > 0) {
       const uint64_t more = idx < 64 ? __builtin_amdgcn_ballot_w64(win.units > 0) & (~0ull << idx) : 0;
       if (more == 0) {
@@ -353,23 +362,10 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
       }
       idx = __builtin_ctzll(more);
       const int units = lane_of(win.units, idx), cost = p.piece_units;
-      int take, t0, t1;
-      bool ends = true;          // whether the request's units do
-      if constexpr (kSeen<Args>) {
-        const int per = lane_of(win.tiles, idx) + cost;
-        q.block = units > per ? skip / per : 0;
-        const int off = skip - q.block * per;
-        take = per - off < left ? per - off : left;
-        t0 = off > cost ? off - cost : 0, t1 = off + take > cost ? off + take - cost : 0;
-        skip += take;
-        ends = skip >= units;
-        if (ends) skip = 0;
-      } else {
-        take = units - skip < left ? units - skip : left;
-        t0 = skip > cost ? skip - cost : 0, t1 = skip + take > cost ? skip + take - cost : 0;
-        skip = 0;
-      }
+      const int take = units - skip < left ? units - skip : left;
+      const int t0 = skip > cost ? skip - cost : 0, t1 = skip + take > cost ? skip + take - cost : 0;
       left -= take;
+      skip = 0;
       if (t1 > t0) {
         q.b = base + idx;
         q.rows = lane_of(win.rows, idx);
@@ -383,10 +379,10 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
         q.count = q.tiles <= ws ? 0 : (q.tiles - ws + STREAMS - 1) / STREAMS;
         q.sight = sight_of(p, q.rows, q.end, q.len);
         q.ids = pages_of(q, 0);
-        if (ends) ++idx;
+        ++idx;
         break;
       }
-      if (ends) ++idx;
+      ++idx;
     }
     left = one(left);
     idx = one(idx);
@@ -467,7 +463,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   // Queries of a piece: B operand of k-step s, row lr, the chunk of 8 channels that K's lanes hold there
   bf16x8_t qop[kSteps];
   auto load_q = [&](const Piece &q) {
-    const int lane = hidden(thread & 63), r = kCacheRowBlock * q.block + NR * half + lane % NR, lq = lane / NR;
+    const int lane = hidden(thread & 63), r = NR * half + lane % NR, lq = lane / NR;
     const int i = (int)((uint32_t)r * p.g_inv >> 16);      // r / G
     const int64_t row = (int64_t)q.row0 + i;
     const bool ok = r < q.rows * p.G && row >= 0 && row < p.num_rows;
@@ -557,8 +553,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
   }
 
   while (true) {
-    const int n = cp.rows, first_row = kCacheRowBlock * cp.block, M = kSeen<Args> && n * p.G - first_row > kCacheRowBlock ? kCacheRowBlock : n * p.G - first_row;
-    const int len = cp.len, row0 = cp.row0, end = cp.end, h = cp.h, t0 = cp.t0;
+    const int n = cp.rows, M = n * p.G, len = cp.len, row0 = cp.row0, end = cp.end, h = cp.h, t0 = cp.t0;
     int tx = hidden(thread);
     const int lane = tx & 63, lr = lane % NR;
     uint32_t hole = gone;      // of the tile that x belongs to
@@ -566,7 +561,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     load_tile(1);
 
     Seen seen;
-    if constexpr (kSeen<Args>) seen = seen_by(p, n, row0, end, len, (int)((uint32_t)(first_row + NR * half + lr) * p.g_inv >> 16));
+    if constexpr (kSeen<Args>) seen = seen_by(p, n, row0, end, len, (int)((uint32_t)(NR * half + lr) * p.g_inv >> 16));
     // tokens that the lane's row sees, and that every row sees
     const int64_t last = (int64_t)end - n + 1 + (int)((uint32_t)(NR * half + lr) * p.g_inv >> 16);
     const int limit = p.causal && last < len ? (last < 0 ? 0 : (int)last) : len;
@@ -711,8 +706,8 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
     auto finish = [&](int r, int seg, auto segs, float m, float l, auto piece_at) {
       constexpr int kSegs = decltype(segs)::value, kPieces = kCacheDim / 4 / kSegs;
       if (cp.tiles == cp.whole) {
-        const int rb = first_row + r, i = (int)((uint32_t)rb * p.g_inv >> 16);
-        const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + rb - i * p.G;
+        const int i = (int)((uint32_t)r * p.g_inv >> 16);
+        const int64_t row = ((int64_t)row0 + i) * p.Hq + h * p.G + r - i * p.G;
         if (row0 + i >= 0 && row0 + i < p.num_rows) {
           const RowEnd end = row_end(p, row, m, l);
 #pragma unroll
@@ -724,7 +719,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(FMT, NR)) void cache_attend_
         }
       } else {
         // two states per worker at most: of a pair that starts before the share, and of one that ends behind it
-        const int64_t o = (int64_t)(2 * worker + (t0 == 0 ? 1 : 0)) * part_rows(p) + r;
+        const int64_t o = (int64_t)(2 * worker + (t0 == 0 ? 1 : 0)) * p.M + r;
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) *reinterpret_cast<f32x4_t *>(p.part_a + o * kCacheDim + 4 * (seg + kSegs * k)) = piece_at(k);
         if (seg == 0) *reinterpret_cast<f32x2_t *>(p.part_ml + 2 * o) = f32x2_t{m, l};
@@ -855,7 +850,7 @@ CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M) {
   r.alone = M <= 32 && pairs >= 256 * kWaves;
   r.piece_units = r.alone ? kPieceAlone : kPieceGroup;
   const int64_t most = 256 * waves * (r.alone ? kWaves : 1);
-  const int64_t units = pairs * cache_row_blocks(M) * ((capacity + kCacheTile - 1) / kCacheTile + r.piece_units);
+  const int64_t units = pairs * ((capacity + kCacheTile - 1) / kCacheTile + r.piece_units);
   const int64_t need = (units + kMinShare - 1) / kMinShare;
   r.workers = (int)(need < most ? need : most);
   return r;

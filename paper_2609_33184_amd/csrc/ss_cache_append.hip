@@ -24,6 +24,10 @@ namespace {
 // by 7e-12; the turned pair.  That is rounded to fp32 and then to bf16, as a
 // reference in 64 bits rounds it; K is quantised from there, so that a cache is bit
 // for bit the one that the rotated rows' ss_cache_write gives.
+//
+// What bounds it: filling prompts, memory (16 of 2048 to 8191 rows, 32 + 8 heads, 8 bits: 1.7 GB read and
+// written, 389 us, 4.3 TB/s; a large copy 4.9); drafted rows the angles' 30 products of 64 bits each and a launch (16 requests of 16
+// to 48 rows, 64 + 8 heads in bf16 8.4 us; every lane its own eight angles 10.3).
 // ---------------------------------------------------------------------------
 
 // cos and sin of p f.
@@ -174,7 +178,8 @@ hipError_t append(const CacheAppendArgs &p, hipStream_t s) {
 // Keeping a path.  Of a request's last n tokens the kept ones move to the first
 // places, whole rows with their scales, so nothing is rounded.  A workgroup takes
 // one request and KV head and has read all of them (at most kCacheMaxTree, 16 lanes
-// a row) before it writes one, whatever order they are given in.
+// a row) before it writes one, whatever order they are given in.  Its time is one round
+// trip to memory behind the table's and the list's: 256 requests, up to 12 rows each of 8 heads in bf16 (7 MB) 6.1 us, one request 3.2.
 // ---------------------------------------------------------------------------
 template <int BYTES>
 struct Bytes;

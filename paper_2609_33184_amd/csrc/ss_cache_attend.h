@@ -16,11 +16,11 @@ constexpr int kMinShare = 4;                        // units: 300 tokens 7.5 us,
 // `sinks` and those behind them and the gap are attended.
 template <typename Args>
 constexpr bool kSeen = std::is_base_of_v<CacheSeenArgs, Args>;
-// Tokens of a tile, and rows of one KV head that a piece holds at most (SeenArgs).
+// Tokens of a tile, and rows of one KV head that a piece holds at most.
 template <typename Args>
 constexpr int kTileOf = std::is_same_v<Args, CacheGroupArgs> ? kCacheGroupTile : kCacheTile;
 template <typename Args>
-constexpr int kBlockOf = std::is_same_v<Args, CacheGroupArgs> ? kCacheGroupBlock : kCacheRowBlock;
+constexpr int kBlockOf = std::is_same_v<Args, CacheGroupArgs> ? kCacheGroupBlock : kCacheMaxRows;
 struct Sight {
   int sinks, gap;
 };
@@ -42,13 +42,13 @@ __device__ __forceinline__ Sight sight_of(const Args &p, int rows, int end, int 
 // Blocks that a request's rows of one KV head are attended in.
 template <typename Args>
 __device__ __forceinline__ int row_blocks(const Args &p, int rows) {
-  if constexpr (kSeen<Args>) return (rows * p.G + kBlockOf<Args> - 1) / kBlockOf<Args>;
+  if constexpr (std::is_same_v<Args, CacheGroupArgs>) return (rows * p.G + kCacheGroupBlock - 1) / kCacheGroupBlock;
   return 1;
 }
 // Rows of a piece's state.
 template <typename Args>
 __device__ __forceinline__ int part_rows(const Args &p) {
-  return kSeen<Args> && p.M > kBlockOf<Args> ? kBlockOf<Args> : p.M;
+  return p.M < kBlockOf<Args> ? p.M : kBlockOf<Args>;
 }
 
 // A request as the attention needs it; in a window, lane i holds request base + i.

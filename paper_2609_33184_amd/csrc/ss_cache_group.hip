@@ -1,5 +1,35 @@
 // gfx950 (MI355X) attention of many query rows per KV head over the paged cache:
 // trees of drafted tokens.
+//
+// o = sum_t softmax(s)_t v_t over the tokens that a row sees, s_t = scale q k_t; one pass over the tiles with a
+// running maximum and sum per row.  In cache_attend_kernel each wave brings, decodes
+// and stages its own tiles for 32 rows; with more rows the decoding of K and V and the bytes are
+// paid again and again.  Here a workgroup's four waves hold 128 rows of a KV head (32
+// each; up to 64 rows: two waves for either half of the tiles) and share each
+// tile of 32 tokens: it is decoded once into LDS, 16 bits a value, K in the rows' order and V
+// for its transpose read, four tiles deep, with one barrier a tile.  More than 128 rows are attended
+// in blocks of 128, which neighbouring workers of one XCD take, so that the second
+// reading of K and V comes from the L2.  The work is cut as in cache_attend_kernel.
+//
+// Per wave and tile: 8 v_mfma_f32_32x32x16 for S^T = K Q^T of the next tile, beside this tile's
+// softmax, and 16 (V in 8 or 4 bits) or 24 (bf16) for O^T += V^T P^T, interleaved with
+// the vector work by hand.
+//
+// Precision.  bf16: P in three parts of bf16, exact, as in cache_attend_kernel.  8 and 4 bits: V's code times
+// scale times 2^8 is an exact f16 number while the scale lies in [2^-23, 2^-1] (e4m3) or
+// [2^-31, 2^5] (e2m1), and P, at most 2^8 and times 2^7, is cut into two f16 numbers, 22 bits or 2^-25: a
+// third less matrix work than three parts (16 x 32768 tokens, 96 rows: 547 us, in three parts 707
+// by waves for themselves).  A tile with other scales, or values that are no numbers, is attended token by token in
+// fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
+//
+// bf16 rows go from memory to LDS without passing registers.  What a wave needs next is waited for by
+// count, so that the loads behind it stay in flight.
+//
+// What bounds it.  bf16, 16 x 12000..16384 tokens, 256 rows: 520 us; the SIMDs issue vector work 45% and
+// matrix work 47% of the cycles, one after the other, at 1.65 GHz; the matrix work alone would take 185 us of the formula and
+// twice that in three parts.  8 bits, 16 x 32768 tokens, 96 rows: 551 us, 155 for the bytes; vector work 37%,
+// matrix work 31% on three SIMDs of four (96 rows leave a wave without), the rest waits at the barrier and for LDS.  One
+// request of 32768 tokens, 256 rows: 92 us and 10.5 for the join of its 32 states a row.
 #include <hip/hip_runtime.h>
 
 #include "ss_cache.h"
@@ -19,7 +49,7 @@ constexpr int kBuffers = 4;                     // tiles in LDS
 constexpr int kSteps = kCacheDim / 16;          // of a product over the channels
 constexpr int kAccs = kCacheDim / 32;           // accumulators of 32 channels
 
-// What a piece costs beside its tiles, in tiles.
+// What a piece costs beside its tiles, in tiles: 24 ragged requests with 4, 8 and 16 52.7, 53.4 and 63.6 us.
 constexpr int kPieceGroupTiles = 8;
 
 // Half precision for P and V.  V's values times 2^kVShift are exact numbers of it if

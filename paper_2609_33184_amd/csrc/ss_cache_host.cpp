@@ -82,7 +82,7 @@ ss_status check_tree_desc(const ss_cache_desc *d) {
     return fail(SS_ERR_UNSUPPORTED, "max_rows x num_q_heads %d x %d > 32768", d->max_rows, d->num_q_heads);
   // tiles of all requests, heads and blocks of rows are counted in 32 bits
   const int64_t tiles = ((int64_t)d->table_stride * d->page_tokens + ss::kCacheTile - 1) / ss::kCacheTile * d->num_requests;
-  const int blocks = ss::cache_row_blocks(d->max_rows * (d->num_q_heads / d->num_kv_heads));
+  const int blocks = (d->max_rows * (d->num_q_heads / d->num_kv_heads) + ss::kCacheGroupBlock - 1) / ss::kCacheGroupBlock;
   if (tiles > (int64_t(1) << 30) / d->num_kv_heads / blocks)
     return fail(SS_ERR_UNSUPPORTED, "num_requests x table_stride x num_kv_heads x %d blocks of rows reaches more than 2^35 tokens", blocks);
   return SS_OK;
@@ -143,18 +143,21 @@ void fill(ss::CacheArgs *p, const ss_cache_desc *d, const void *pages, const int
   p->max_rows = d->max_rows;
 }
 
+static_assert(ss::kCacheMaxRows == SS_MAX_ROWS_PER_KV_HEAD, "more rows are attended in groups");
+
 struct AttendLayout {
-  int M;
+  int M, blocks;      // rows per KV head, and the blocks that they are attended in
   bool group;         // attended by the kernel of many rows
   ss::CacheSplit split;
   size_t ml, bytes;   // offset of the maxima and sums; all of it
   explicit AttendLayout(const ss_cache_desc *d, bool grouped = false) {      // grouped: many rows may be
     M = d->max_rows * (d->num_q_heads / d->num_kv_heads);
     group = grouped && M >= ss::cache_group_rows(d->format);
-    const int reach = d->table_stride * d->page_tokens, block = group ? ss::kCacheGroupBlock : ss::kCacheRowBlock;
+    const int reach = d->table_stride * d->page_tokens;
+    blocks = group ? (M + ss::kCacheGroupBlock - 1) / ss::kCacheGroupBlock : 1;
     split = group ? ss::cache_group_split(d->format, d->num_requests, d->num_kv_heads, reach, M)
                   : ss::cache_attend_split(d->format, d->num_requests, d->num_kv_heads, reach, M);
-    const size_t rows = 2 * (size_t)split.workers * (size_t)(M < block ? M : block);
+    const size_t rows = 2 * (size_t)split.workers * (size_t)(blocks > 1 ? ss::kCacheGroupBlock : M);
     ml = rows * ss::kCacheDim * sizeof(float);
     bytes = (ml + rows * 2 * sizeof(float) + 255) / 256 * 256;
   }
@@ -168,7 +171,7 @@ void fill_seen(ss::CacheSeenArgs *p, const ss_cache_desc *d, const AttendLayout 
   int64_t reach = p->capacity;
   // a window's tokens begin and end within a tile, and so do the first ones
   if (window > 0 && (int64_t)window + sinks + d->max_rows < reach) reach = (int64_t)window + sinks + d->max_rows + 3 * ss::kCacheTile;
-  const int block = layout.group ? ss::kCacheGroupBlock : ss::kCacheRowBlock, wholes = p->B * p->Hkv * ((layout.M + block - 1) / block);
+  const int wholes = p->B * p->Hkv * layout.blocks;
   // two workgroups a CU for groups (16 trees of 32 rows in a window of 4096 93 us, one 131), else one (32 requests of one row in a
   // window of 1024 29.5, two 31.0)
   const int fill = layout.group ? 512 : 256, most = p->workers < fill ? p->workers : fill;

@@ -62,7 +62,7 @@ ATTEND = [(dict(num_q_heads=0), "num_q_heads", INVALID), (dict(num_q_heads=9), "
     (dict(max_rows=65), "max_rows", INVALID), (dict(max_rows=64, num_q_heads=18), "rows per KV head", UNSUPPORTED),
     (dict(max_rows=1, num_q_heads=130), "query heads per KV head", UNSUPPORTED),
     (dict(max_rows=64, num_kv_heads=512, num_q_heads=1024, num_requests=1), "max_rows x num_q_heads", UNSUPPORTED),
-    (dict(max_rows=64, num_requests=64, table_stride=1 << 21, num_q_heads=16), "blocks of rows", UNSUPPORTED)], ids=lambda x: str(x)[:40])
+    (dict(max_rows=64, num_requests=256, table_stride=1 << 21, num_q_heads=16), "blocks of rows", UNSUPPORTED)], ids=lambda x: str(x)[:40])
 def test_descriptors_that_a_tree_refuses(kw, word, status):
     d = _desc(**kw)
     assert ss.ss_cache_attend_tree_workspace_bytes(d) == 0 and word in ss.ss_last_error()
