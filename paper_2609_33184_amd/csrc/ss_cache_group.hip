@@ -8,8 +8,8 @@
 // each; up to 64 rows: two waves for either half of the tiles) and share each
 // tile of 32 tokens: it is decoded once into LDS, 16 bits a value, K in the rows' order and V
 // for its transpose read, four tiles deep, with one barrier a tile.  More than 128 rows are attended
-// in blocks of 128, which neighbouring workers of one XCD take, so that the second
-// reading of K and V comes from the L2.  The work is cut as in cache_attend_kernel.
+// in blocks of 128, each of which reads K and V again (16 x 12000..16384 tokens, 256 rows: 1.7 GB of 0.9).  The work is
+// cut as in cache_attend_kernel.
 //
 // Per wave and tile: 8 v_mfma_f32_32x32x16 for S^T = K Q^T of the next tile, beside this tile's
 // softmax, and 16 (V in 8 or 4 bits) or 24 (bf16) for O^T += V^T P^T, interleaved with
@@ -122,8 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   __shared__ Piece ring[kWaves][8];                        // the pieces on their way
   const int thread = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(thread >> 6);
-  // neighbouring workers, which may attend the same tiles for other rows, on one XCD
-  const int worker = p.workers % 8 == 0 ? (int)(blockIdx.x % 8) * (p.workers / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
+  const int worker = blockIdx.x;
   auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
 
   // This worker's share and where it starts, as in cache_attend_kernel.
