@@ -17,9 +17,9 @@
 //
 // Precision.  bf16: P in three parts of bf16, exact, as in cache_attend_kernel.  8 and 4 bits: V's code times
 // scale times 2^8 is an exact f16 number while the scale lies in [2^-23, 2^-1] (e4m3) or
-// [2^-31, 2^5] (e2m1), and P, at most 2^8 and times 2^7, is cut into two f16 numbers, 22 bits or 2^-25: a
-// third less matrix work than three parts (16 x 32768 tokens, 96 rows: 547 us, in three parts 707
-// by waves for themselves).  A tile with other scales, or values that are no numbers, is attended token by token in
+// [2^-31, 2^5] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or 2^-38 of the largest
+// weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 547 us, in three parts 707
+// by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  A tile with other scales, or values that are no numbers, is attended token by token in
 // fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
 //
 // bf16 rows go from memory to LDS without passing registers.  What a wave needs next is waited for by
@@ -53,8 +53,10 @@ constexpr int kAccs = kCacheDim / 32;           // accumulators of 32 channels
 constexpr int kPieceGroupTiles = 8;
 
 // Half precision for P and V.  V's values times 2^kVShift are exact numbers of it if
-// their blocks' exponents lie in [kLeast, kMost]; P's maximum is 2^kPShift times 2^kSlack.
-constexpr int kVShift = 8, kPShift = 7;
+// their blocks' exponents lie in [kLeast, kMost]; P's maximum is 2^kPShift times 2^kHalfSlack: a
+// long tail of weights below 2^-26 of f16 would be lost as a whole.
+constexpr int kVShift = 8, kPShift = 12;
+constexpr float kHalfSlack = 3.f;
 template <int FMT>
 struct Half {      // bounds of a scale byte
   static constexpr uint32_t kLeast = 127 - (FMT == kCacheMx8 ? 23 : 31), kMost = 127 + (FMT == kCacheMx8 ? -1 : 5);
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
 #pragma unroll
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[e]);
       mx *= p.scale_log2;
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_run + kSlack) != 0, 0)) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_run + (kHalf ? kHalfSlack : kSlack)) != 0, 0)) {
         const float mn = fmaxf(m_run, xgroup_max<2>(mx));
         const float alpha = mn == kNegInf ? 1.f : exp2_fast(m_run - mn);
         l_run *= alpha;

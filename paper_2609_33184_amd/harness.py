@@ -584,6 +584,13 @@ class PagedCache:
         return (out.data_ptr(), None if lse is None else lse.data_ptr(), None if prev is None else prev[0].data_ptr(),
                 None if prev is None else prev[1].data_ptr())
 
+    @staticmethod
+    def _window(window: int, sinks: int) -> Tuple[int, int]:
+        window, sinks = operator.index(window), operator.index(sinks)
+        if not 0 <= window < 2 ** 31 or not 0 <= sinks < 2 ** 31 or sinks > 0 and window == 0:
+            raise ValueError(f"window and sinks are 0 or more and fit 31 bits, sinks with a window only (got {window}, {sinks})")
+        return window, sinks
+
     def attend(self, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], stream: int,
                row_start: Optional[torch.Tensor] = None, prev: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
                window: int = 0, sinks: int = 0) -> None:
@@ -592,8 +599,7 @@ class PagedCache:
         stride = self._row_stride(q, self.desc.num_q_heads)
         to, to_lse, prev_out, prev_lse = self._results(q, out, lse, prev)
         starts = self._starts(row_start)
-        if window < 0 or sinks < 0 or sinks > 0 and window == 0:
-            raise ValueError(f"window and sinks are 0 or more, sinks with a window only (got {window}, {sinks})")
+        window, sinks = self._window(window, sinks)
         on = self._begins(stream, True)
         if window == 0:
             ss.ss_cache_attend(self.desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0],
@@ -618,8 +624,7 @@ class PagedCache:
             raise ValueError(f"tree is a packed int64 or uint64 [{q.shape[0]}] on {self.pages.device}")
         to, to_lse, prev_out, prev_lse = self._results(q, out, lse, prev)
         starts = self._starts(row_start)
-        if window < 0 or sinks < 0 or sinks > 0 and window == 0:
-            raise ValueError(f"window and sinks are 0 or more, sinks with a window only (got {window}, {sinks})")
+        window, sinks = self._window(window, sinks)
         on = self._begins(stream, True)
         ss.ss_cache_attend_tree(desc, self.pages.data_ptr(), self.table.data_ptr(), q.data_ptr(), q.shape[0], self.end.data_ptr(),
                                 tree.data_ptr(), to, to_lse, starts, window, sinks, prev_out, prev_lse,

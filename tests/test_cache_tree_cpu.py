@@ -255,7 +255,8 @@ def test_paged_cache_attentions(reached):
     p.attend_tree(q, tree, out, lse, 0, prev=(out, lse), window=5)
     p.attend_tree(q, tree.view(torch.uint64), out, lse, 0)
     assert [c[0] for c in reached] == ["ss_cache_attend", "ss_cache_attend_window", "ss_cache_attend_tree", "ss_cache_attend_tree"]
-    for call in (lambda: p.attend(q, out, lse, 0, window=-1), lambda: p.attend(q, out, lse, 0, sinks=1), lambda: p.attend(q, out, lse, 0, window=2, sinks=-1),
+    for call in (lambda: p.attend(q, out, lse, 0, window=2 ** 32 + 5), lambda: p.attend_tree(q, tree, out, lse, 0, window=2 ** 31),
+                 lambda: p.attend(q, out, lse, 0, window=4, sinks=2 ** 33), lambda: p.attend(q, out, lse, 0, window=-1), lambda: p.attend(q, out, lse, 0, sinks=1), lambda: p.attend(q, out, lse, 0, window=2, sinks=-1),
                  lambda: p.attend_tree(q, tree, out, lse, 0, sinks=4), lambda: p.attend_tree(q, tree[:7], out, lse, 0),
                  lambda: p.attend_tree(q, tree.int(), out, lse, 0), lambda: p.attend_tree(q, [0] * 8, out, lse, 0),
                  lambda: p.attend_tree(q, torch.zeros(16, dtype=torch.int64)[::2], out, lse, 0),

@@ -440,6 +440,24 @@ def test_tree_values_near_the_largest(fmt, hq, n, where):
     assert np.abs(r.lse.cpu().numpy() - wl).max() <= 5e-6 * max(1.0, np.abs(wl).max())
 
 
+@pytest.mark.parametrize("fmt", FORMATS, ids=IDS.get)
+@pytest.mark.parametrize("hq,n", ((8, 7), (8, 40), (16, 64)))
+@pytest.mark.parametrize("gap", (18, 24, 27))
+def test_tree_long_tail(fmt, hq, n, gap):
+    """A first token that outweighs each other by e^gap, whose values the others' are 256 times: with gap 24 each of 6000 tokens
+    weighs 2^-34.6 and all their values make 6e-5 of the result, which the sum of what is small must not lose."""
+    rng = np.random.default_rng(n)
+    end = [6000 + n]
+    q = torch.full((n, hq, 128), 1.0).to(torch.bfloat16) + 0.25 * _normal(4, n, hq, 128).cpu()
+    k = 0.25 * _normal(5, sum(end), 2, 128)
+    k[0] = gap / 128 ** 0.5
+    v = 256 * (1 + 0.25 * _normal(6, sum(end), 2, 128).float()).to(torch.bfloat16)
+    v[0] = 1.0
+    c = Cache(fmt, 2, 32, end)
+    c.fill_tokens(end, 5, k, v)
+    TreeRows(c, hq, _trees(rng, (n,)), end, q=q.cuda().to(torch.bfloat16).contiguous()).run().check()
+
+
 @pytest.mark.parametrize("hq,n", ((4, 7), (8, 40), (8, 64)))
 def test_tree_codes_that_are_no_numbers(hq, n):
     """An e4m3 code that is none, under an ordinary scale, in a node's V: rows that do not see it stay as they are."""
@@ -799,6 +817,37 @@ def test_tree_step_in_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(got, (c.dev, qt, out, lse)))
         ends = [e + len(x) for e, x in zip(ends, paths)]
+
+
+def test_window_in_a_graph():
+    """A captured call goes on with other lengths: parts without tiles, of requests that grow past the window."""
+    end = [2500, 700, 3, 0]
+    rows = [4, 2, 3, 1]
+    c = Cache(oc.MXFP8, 2, 32, end, width=96)
+    c.fill_tokens(end, 5)
+    r = WindowRows(c, 32, rows, end, 600, 30)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        r.run(side)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.run()
+    for shorter in ([0, 0, 0, 0], [2490, 699, 3, 0], [1, 640, 0, 0], [400, 0, 2, 0]):
+        r.end = [e - s for e, s in zip(end, shorter)]
+        r.dend.copy_(_ints(r.end))
+        r.out.fill_(7.0)
+        r.lse.fill_(7.0)
+        r.ws.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        out, lse = r.out.clone(), r.lse.clone()
+        r.check()
+        r.run()
+        torch.cuda.synchronize()
+        assert torch.equal(out, r.out) and torch.equal(lse, r.lse)
 
 
 def test_tree_pages_beyond_32_bits_on_another_stream():
