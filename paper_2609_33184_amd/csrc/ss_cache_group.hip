@@ -18,7 +18,7 @@
 // Precision.  bf16: P in three parts of bf16, exact, as in cache_attend_kernel.  8 and 4 bits: V's code times
 // scale times 2^8 is an exact f16 number while the scale lies in [2^-23, 2^-1] (e4m3) or
 // [2^-31, 2^5] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or 2^-38 of the largest
-// weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 547 us, in three parts 707
+// weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 540 us, in three parts 707
 // by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  A tile with other scales, or values that are no numbers, is attended token by token in
 // fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
 //
@@ -27,7 +27,7 @@
 //
 // What bounds it.  bf16, 16 x 12000..16384 tokens, 256 rows: 520 us; the SIMDs issue vector work 45% and
 // matrix work 47% of the cycles, one after the other, at 1.65 GHz; the matrix work alone would take 185 us of the formula and
-// twice that in three parts.  8 bits, 16 x 32768 tokens, 96 rows: 551 us, 155 for the bytes; vector work 37%,
+// twice that in three parts.  8 bits, 16 x 32768 tokens, 96 rows: 540 us, 155 for the bytes; vector work 37%,
 // matrix work 31% on three SIMDs of four (96 rows leave a wave without), the rest waits at the barrier and for LDS.  One
 // request of 32768 tokens, 256 rows: 92 us and 10.5 for the join of its 32 states a row.
 #include <hip/hip_runtime.h>
@@ -289,8 +289,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
       const uint64_t run = run_at(mine);
       const uint64_t scales = run + ks_off - (uint32_t)((tok + 16 * mine) & (page_tokens - 1)) * (kRow - 4);
       gone[set] = tok + kTokens > len || hole != 0 ? __builtin_amdgcn_ballot_w64(tok + 16 * mine + r >= len || ((hole >> mine) & 1u) != 0) : 0;
-      auto rows = [&](uint64_t at) { return *(const u32x4_t *)((const uint8_t *)at + (uint32_t)(r * kRow + 16 * (tx % kLanes))); };
-      auto scale = [&](uint64_t at) { return (uint32_t)*((const uint8_t *)at + (uint32_t)(4 * r + tx % kLanes * 4 / kLanes)); };
+      // said to be global: a load that might be of LDS is waited for at every barrier
+      using Bytes = const __attribute__((address_space(1))) uint8_t *;
+      auto rows = [&](uint64_t at) { return *(const __attribute__((address_space(1))) u32x4_t *)((Bytes)at + (uint32_t)(r * kRow + 16 * (tx % kLanes))); };
+      auto scale = [&](uint64_t at) { return (uint32_t)*((Bytes)at + (uint32_t)(4 * r + tx % kLanes * 4 / kLanes)); };
       if constexpr (FMT == kCacheMx8) {
         kr[set] = rows(run);
         vr[set] = rows(run + v_off);
