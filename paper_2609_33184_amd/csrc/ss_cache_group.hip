@@ -16,11 +16,11 @@
 // the vector work by hand.
 //
 // Precision.  bf16: P in three parts of bf16, exact, as in cache_attend_kernel.  8 and 4 bits: V's code times
-// scale times 2^8 is an exact f16 number while the scale lies in [2^-23, 2^-1] (e4m3) or
-// [2^-31, 2^5] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or 2^-38 of the largest
+// scale times 2^6 or 2^2 is an exact f16 number while the scale lies in [2^-21, 2] (e4m3) or
+// [2^-25, 2^11] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or 2^-38 of the largest
 // weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 540 us, in three parts 707
-// by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  A tile with other scales, or values that are no numbers, is attended token by token in
-// fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
+// by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  A tile with other
+// scales, or values that are no numbers, is attended token by token in fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
 //
 // bf16 rows go from memory to LDS without passing registers.  What a wave needs next is waited for by
 // count, so that the loads behind it stay in flight.
@@ -53,13 +53,16 @@ constexpr int kAccs = kCacheDim / 32;           // accumulators of 32 channels
 constexpr int kPieceGroupTiles = 8;
 
 // Half precision for P and V.  V's values times 2^kVShift are exact numbers of it if
-// their blocks' exponents lie in [kLeast, kMost]; P's maximum is 2^kPShift times 2^kHalfSlack: a
-// long tail of weights below 2^-26 of f16 would be lost as a whole.
-constexpr int kVShift = 8, kPShift = 12;
+// their blocks' scale bytes lie in [kLeast, kMost]: blocks of e4m3 whose largest value lies between 2^-13 and 896, and of e2m1
+// between 2^-23 and 12288.  P's maximum is 2^kPShift times 2^kHalfSlack: a long tail of weights below 2^-26 of f16 would
+// be lost as a whole.
+constexpr int kPShift = 12;
 constexpr float kHalfSlack = 3.f;
 template <int FMT>
-struct Half {      // bounds of a scale byte
-  static constexpr uint32_t kLeast = 127 - (FMT == kCacheMx8 ? 23 : 31), kMost = 127 + (FMT == kCacheMx8 ? -1 : 5);
+struct Half {
+  // least and largest magnitude of a code but 0: 2^-9 and 448, 1/2 and 6; of an f16 number 2^-24 and 65504
+  static constexpr int kVShift = FMT == kCacheMx8 ? 6 : 2;
+  static constexpr uint32_t kLeast = 127 - (FMT == kCacheMx8 ? 15 : 23) - kVShift, kMost = 127 + (FMT == kCacheMx8 ? 7 : 13) - kVShift;
 };
 
 // Scale bytes beyond which V's sums might pass the largest number with these factors: from such a tile on a piece goes without.
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
     constexpr int set = decltype(parity)::value;
     const uint32_t to = (uint32_t)(uintptr_t)smem[number & (kBuffers - 1)][0];
     if constexpr (FMT == kCacheMx8) {
-      const float kf = scale_of(ks[set]), vf = scale_of(vs[set] + (exact ? 0 : kVShift));
+      const float kf = scale_of(ks[set]), vf = scale_of(vs[set] + (exact ? 0 : Half<FMT>::kVShift));
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const u32x2_t a = widen8(kr[set][2 * j], kf), d = widen8(kr[set][2 * j + 1], kf);
@@ -336,7 +339,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
       }
     } else if constexpr (FMT == kCacheMx4) {
       const bool half = w >= 2 && !exact;
-      const float f = scale_of(vs[set] + (half ? kVShift : 0));
+      const float f = scale_of(vs[set] + (half ? Half<FMT>::kVShift : 0));
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t x = kr[set][j];
@@ -561,14 +564,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
           plain = true;
           l_run *= 1.f / (1 << kPShift);
 #pragma unroll
-          for (int a = 0; a < kAccs; ++a) acc[a] *= 1.f / (1 << (kPShift + kVShift));
+          for (int a = 0; a < kAccs; ++a) acc[a] *= 1.f / (1 << (kPShift + Half<FMT>::kVShift));
         }
       }
       const float ms = m_run == kNegInf ? 0.f : kHalf && !plain ? m_run - kPShift : m_run;
 
       if (kHalf && __builtin_expect(exact || plain, 0)) {
         // V beyond half precision, which may be no number: each token is added to the rows that see it
-        const float factor = exact ? plain ? 1.f : (float)(1 << kVShift) : 1.f / (1 << kVShift);
+        const float factor = exact ? plain ? 1.f : (float)(1 << Half<FMT>::kVShift) : 1.f / (1 << Half<FMT>::kVShift);
 #pragma unroll 1
         for (int t = 0; t < 32; ++t) {
           const int e = 4 * (t >> 3) + (t & 3);
@@ -678,7 +681,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
       float m = kHalf && !plain ? m_run - kPShift : m_run, l = xgroup_sum<2>(l_run);
 #pragma unroll
       for (int a = 0; a < kAccs; ++a)
-        if constexpr (kHalf) acc[a] *= plain ? 1.f : 1.f / (1 << kVShift);
+        if constexpr (kHalf) acc[a] *= plain ? 1.f : 1.f / (1 << Half<FMT>::kVShift);
       auto piece_of = [&](int c) {
         return f32x4_t{acc[c >> 2][4 * (c & 3)], acc[c >> 2][4 * (c & 3) + 1], acc[c >> 2][4 * (c & 3) + 2], acc[c >> 2][4 * (c & 3) + 3]};
       };

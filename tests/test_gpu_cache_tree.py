@@ -140,6 +140,21 @@ def test_window_parts(fmt, hkv, window, tree):
     assert torch.equal(first, r.out)
 
 
+@pytest.mark.parametrize("hkv,hq,tree,window", ((2, 8, 0, 600), (1, 16, 1, 600), (2, 64, 0, 40), (1, 8, 1, 100)))
+def test_window_parts_of_many_requests(hkv, hq, tree, window):
+    """More than 64 requests, most of them short or empty, a workgroup to each (request, head) and block of rows."""
+    rng = np.random.default_rng(window)
+    B = 131
+    end = rng.integers(0, 40, B) * (rng.random(B) < 0.7)
+    end[[3, 63, 64, 130]] = 1400, 33, 900, 1200
+    rows = rng.integers(0, 13 if tree else 3, B)
+    rows[[3, 64, 130]] = (12, 11, 9) if tree else (2, 1, 2)
+    c = Cache(oc.MXFP8, hkv, 32, end)
+    c.fill_tokens(end, 3)
+    r = TreeRows(c, hq, _trees(rng, rows), end, window, 7, extra=2) if tree else WindowRows(c, hq, rows, end, window, 7, extra=2)
+    r.run().check()
+
+
 def test_window_of_everything_equals_plain_attention():
     """No token is hidden and none skipped: the same tiles in the same shares give the same bits."""
     end, rows = [700, 33, 0, 64], [3, 1, 2, 4]
