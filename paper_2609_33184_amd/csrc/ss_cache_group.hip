@@ -403,11 +403,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   if (lp.tiles == 0) return;
   if (thread < kBuffers) wide[thread] = huge[thread] = spoilt[thread] = -1;
   workgroup_barrier();
-  int exacts = kHalf ? 0 : -1;      // bit i % kBuffers: tile i's V is bf16
+  int exacts = kHalf ? 0 : -1;      // bit i % kBuffers: tile i's V is bf16; kBuffers bits on: beyond kHuge (what was told is gone by then)
   auto bring = [&](auto parity, int number) {      // tile `number` from registers into LDS, behind the barrier that follows its tell
     if (number < issued) {
       const bool exact = one(wide[number & (kBuffers - 1)]) == number;
-      exacts = (exacts & ~(1 << (number & (kBuffers - 1)))) | (exact ? 1 << (number & (kBuffers - 1)) : 0);
+      const bool far = exact && one(huge[number & (kBuffers - 1)]) == number;
+      exacts = (exacts & ~((1 << kBuffers | 1) << (number & (kBuffers - 1)))) | (exact ? (far ? 1 << kBuffers | 1 : 1) << (number & (kBuffers - 1)) : 0);
       if (__builtin_expect(exact, 0))
         stage(parity, number, true);
       else
@@ -560,7 +561,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
         m_run = mn;
       }
       if (kHalf && __builtin_expect(exact, 0)) {
-        if (!plain && one(huge[buf]) == number) {
+        if (!plain && ((exacts >> (kBuffers + buf)) & 1) != 0) {
           plain = true;
           l_run *= 1.f / (1 << kPShift);
 #pragma unroll
