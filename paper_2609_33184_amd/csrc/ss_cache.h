@@ -98,7 +98,7 @@ struct CacheSplit {
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
 // From how many rows per KV head on the rows of a tree are attended in groups, and how that is split.
 // 16 x 32768 tokens with 40 and 64 rows in bf16 450 and 468 us, with waves for themselves 495 and 513; in 8
-// bits 523 and 525, 354 and 371; 96 rows 537 and 707.
+// bits 523 and 525, 354 and 371; 96 rows 530 and 707.
 constexpr int cache_group_rows(int fmt) { return fmt == kCacheBf16 ? 33 : 65; }
 CacheSplit cache_group_split(int fmt, int B, int Hkv, int capacity, int M);
 // Into how many parts of as many tiles (of 32 tokens) each of `wholes` (request, KV head, block of rows) is cut, a workgroup to a

@@ -18,7 +18,7 @@
 // Precision.  bf16: P in three parts of bf16, exact, as in cache_attend_kernel.  8 and 4 bits: V's code times
 // scale times 2^6 or 2^2 is an exact f16 number while the scale lies in [2^-21, 2] (e4m3) or
 // [2^-25, 2^11] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or 2^-38 of the largest
-// weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 540 us, in three parts 707
+// weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 530 us, in three parts 707
 // by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  A tile with other
 // scales, or values that are no numbers, is attended token by token in fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
 //
@@ -27,7 +27,7 @@
 //
 // What bounds it.  bf16, 16 x 12000..16384 tokens, 256 rows: 520 us; the SIMDs issue vector work 45% and
 // matrix work 47% of the cycles, one after the other, at 1.65 GHz; the matrix work alone would take 185 us of the formula and
-// twice that in three parts.  8 bits, 16 x 32768 tokens, 96 rows: 540 us, 155 for the bytes; vector work 37%,
+// twice that in three parts.  8 bits, 16 x 32768 tokens, 96 rows: 530 us, 155 for the bytes; vector work 37%,
 // matrix work 31% on three SIMDs of four (96 rows leave a wave without), the rest waits at the barrier and for LDS.  One
 // request of 32768 tokens, 256 rows: 92 us and 10.5 for the join of its 32 states a row.
 #include <hip/hip_runtime.h>
