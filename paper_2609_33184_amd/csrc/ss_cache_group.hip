@@ -8,7 +8,7 @@
 // each; up to 64 rows: two waves for either half of the tiles) and share each
 // tile of 32 tokens: it is decoded once into LDS, 16 bits a value, K in the rows' order and V
 // for its transpose read, four tiles deep, with one barrier a tile.  More than 128 rows are attended
-// in blocks of 128, each of which reads K and V again (16 x 12000..16384 tokens, 256 rows: 1.7 GB of 0.9).  The work is
+// in blocks of 128, each of which reads K and V again (16 x 12000..16384 tokens, 256 rows: 1.8 GB of 0.9).  The work is
 // cut as in cache_attend_kernel.
 //
 // Per wave and tile: 8 v_mfma_f32_32x32x16 for S^T = K Q^T of the next tile, beside this tile's
