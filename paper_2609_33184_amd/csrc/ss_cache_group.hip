@@ -93,9 +93,10 @@ __device__ __forceinline__ void cut2(float p0, float p1, uint32_t &a, uint32_t &
 
 // A wave's 64 x 16 bytes, at `from` + its lanes' offsets, straight into LDS, lane by lane from `to` on (a byte address there,
 // the wave's).  In assembly, since with the builtin every read of LDS waits for all of them; it has no output register,
-// and what reads the bytes is behind a wait and a barrier.
+// and what reads the bytes is behind a wait and a barrier.  The compiler keeps no distances inside assembly: the load needs one
+// wait state behind M0's write, and five behind a vector instruction that may have written its scalar address.
 __device__ __forceinline__ void load_to_lds(const uint8_t *from, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory", "m0");
 }
 
 __device__ __forceinline__ void workgroup_barrier() {      // of what lies in LDS; loads to registers go on
