@@ -17,9 +17,13 @@
 //
 // Precision.  bf16: P in three parts of bf16, exact, as in cache_attend_kernel.  8 and 4 bits: V's code times
 // scale times 2^6 or 2^2 is an exact f16 number while the scale lies in [2^-21, 2] (e4m3) or
-// [2^-25, 2^11] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or 2^-38 of the largest
-// weight's size: a third less matrix work than three parts (16 x 32768 tokens, 96 rows: 530 us, in three parts 707
-// by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  A tile with other
+// [2^-25, 2^11] (e2m1), and P, at most 2^3 and times 2^12, is cut into two f16 numbers, 22 bits or all but 2^-25 of it: a
+// third less matrix work than three parts (16 x 32768 tokens, 96 rows: 550 us, in three parts 707
+// by waves for themselves).  The running maximum is followed closer for it, from 2^3 on instead of 2^8.  Each weight is held to
+// 2^-18 of itself: where a row sees one below 2^-19 of the largest, the wave attends the tile in two or three steps, each over a
+// range of weights and with a reference 2^20 or 2^40 lower, where it stays while the tiles go on so.  Left in one range, thousands of
+// weights of 2^-37 before large values would be lost, 1.5e-3 of a result where the values are 2^16 times the largest weight's.
+// A tile with other
 // scales, or values that are no numbers, is attended token by token in fp32.  Against 64 bits 9e-7, the plain form in fp32 3.2e-6.
 //
 // bf16 rows go from memory to LDS without passing registers.  What a wave needs next is waited for by
@@ -54,10 +58,13 @@ constexpr int kPieceGroupTiles = 8;
 
 // Half precision for P and V.  V's values times 2^kVShift are exact numbers of it if
 // their blocks' scale bytes lie in [kLeast, kMost]: blocks of e4m3 whose largest value lies between 2^-13 and 896, and of e2m1
-// between 2^-23 and 12288.  P's maximum is 2^kPShift times 2^kHalfSlack: a long tail of weights below 2^-26 of f16 would
-// be lost as a whole.
+// between 2^-23 and 12288.  P's maximum is 2^kPShift times 2^kHalfSlack.
 constexpr int kPShift = 12;
 constexpr float kHalfSlack = 3.f;
+// log2 of the least weight, of the largest, that two parts hold well: they leave 2^-25 of P, so 2^-18 of it.  And by how much the
+// reference is lowered for smaller ones: once, or twice, which does for weights of 2^-59.
+constexpr float kHalfLeast = -19.f;
+constexpr int kHalfStep = 20;
 template <int FMT>
 struct Half {
   // least and largest magnitude of a code but 0: 2^-9 and 448, 1/2 and 6; of an f16 number 2^-24 and 65504
@@ -66,7 +73,8 @@ struct Half {
 };
 
 // Scale bytes beyond which V's sums might pass the largest number with these factors: from such a tile on a piece goes without.
-constexpr uint32_t kHuge = 127 + 60;
+// Below, 2^21 tokens' sums are below 2^(15 + 6 + 9 + 20 + 21), and 2^40 times that while small weights are added.
+constexpr uint32_t kHuge = 127 + 20;
 
 template <int I>
 using Int = std::integral_constant<int, I>;
@@ -440,6 +448,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   f32x16_t acc[kAccs], x = f32x16_t{};      // x: the scores of the tile that this wave attends next
   int M = 0, first_row = 0, groups = 1, mine = 0, turn = 0;      // rows of the block; of all, its first; waves per 32 rows; this wave's rows, its tiles
   bool works = false, plain = false;      // whether it has rows; its state goes without the factors of half precision
+  // Half precision: how far m_run, log2 of what the weights are relative to, lies below the largest score, for the sake of
+  // small weights (not if plain).
+  int lift = 0;
   // S^T = K Q^T of a tile: K's rows read, and multiplied.
   auto read_k = [&](int number, int lane, u32x4_t (&kw)[kSteps]) {
     // chunk 2 s + lq of row lr, at (2 s + lq) ^ (lr & 15): s flips bits of the first one's place
@@ -459,6 +470,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
   int place = 0, k = 0, tiles = 0, t0 = 0;      // the attended piece's place in the ring, which tile of it, how many, the first
   int sinks_to = 0, gap = 0, len = 0;           // of its sight; its request's tokens
   int sees_from = 0, sees_to = 0;               // tokens that all its rows see
+  int to_come = 0;                              // ranges of the tile's weights that are still to come, a bit each
   for (int number = 0; number < issued; ++number, ++k) {      // of the tile attended
     const int buf = number & (kBuffers - 1);
     const bool begins = k == tiles;
@@ -500,39 +512,44 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
       m_run = kNegInf;
       l_run = 0.f;
       plain = false;
+      lift = 0;
 #pragma unroll
       for (int a = 0; a < kAccs; ++a) acc[a] = f32x16_t{};
     }
     const int tok = kTokens * (t0 + k + (t0 + k < sinks_to ? 0 : gap));
     const uint32_t hole = (holes >> 2 * (number & 7)) & 3u;
     const bool cut = hole != 0 || tok + kTokens > sees_to || (tok < sees_from && tok + kTokens > p.sinks);      // some rows do not see some of it
-    // in flight stay, straight to LDS, tile i + 2's four loads where tile i + 1 is needed next, else none; to registers all
-    if constexpr (kDirect) {
-      if (groups == 1 && number + 2 < issued)
-        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-      else
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    } else if (number + 3 < issued) {
-      if (number & 1)
-        tell(Int<0>{}, number + 3);
-      else
-        tell(Int<1>{}, number + 3);
-    }
-    workgroup_barrier();
-    const bool exact = (exacts >> buf) & 1;
-    if (kDirect && __builtin_expect(cut, 0)) {
-      clear(number, len - tok, hole);
+    const int pending = to_come;      // not 0: the tile was attended, but for these
+    to_come = 0;
+    if (!kHalf || pending == 0) {
+      // in flight stay, straight to LDS, tile i + 2's four loads where tile i + 1 is needed next, else none; to registers all
+      if constexpr (kDirect) {
+        if (groups == 1 && number + 2 < issued)
+          asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        else
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      } else if (number + 3 < issued) {
+        if (number & 1)
+          tell(Int<0>{}, number + 3);
+        else
+          tell(Int<1>{}, number + 3);
+      }
       workgroup_barrier();
-    }
-    if constexpr (kDirect) {
-      load(Int<0>{});
-    } else {
-      if (number & 1)
-        bring(Int<0>{}, number + 3);
-      else
-        bring(Int<1>{}, number + 3);
+      if (kDirect && __builtin_expect(cut, 0)) {
+        clear(number, len - tok, hole);
+        workgroup_barrier();
+      }
+      if constexpr (kDirect) {
+        load(Int<0>{});
+      } else {
+        if (number & 1)
+          bring(Int<0>{}, number + 3);
+        else
+          bring(Int<1>{}, number + 3);
+      }
     }
 
+    const bool exact = (exacts >> buf) & 1;
     if (begins && works) {      // the first scores of the piece: of its tile 0 or 1
       u32x4_t kw[kSteps];
       read_k(number + turn, hidden(thread & 63), kw);
@@ -540,33 +557,76 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
     }
     // This tile's softmax and products, and the scores of the wave's next tile (of whatever lies there, if that is none)
     if (works && (groups == 1 || (k & 1) == turn)) {
-      const int lane = hidden(thread & 63), lq = lane >> 5;
       uint32_t word = ~0u;       // the tile's tokens that the lane's row sees
+      const int lane = hidden(thread & 63), lq = lane >> 5;
+      float least = -kNegInf;    // the smallest score that is seen
       if (__builtin_expect(cut, 0)) {
         const Piece q = uniform(ring[w][place]);
         const Seen seen = {bits, (int64_t)q.end - q.rows, low, p.sinks, q.len, 0, 0};
         word = seen.word(tok) & (hole & 1u ? 0xffff0000u : ~0u) & (hole & 2u ? 0xffffu : ~0u);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = (word >> (8 * (e >> 2) + 4 * lq + (e & 3))) & 1u ? x[e] : kNegInf;
+        for (int e = 0; e < 16; ++e) {
+          const bool sees = (word >> (8 * (e >> 2) + 4 * lq + (e & 3))) & 1u;
+          if constexpr (kHalf) least = fminf(least, sees ? x[e] : -kNegInf);
+          x[e] = sees ? x[e] : kNegInf;
+        }
+      } else if constexpr (kHalf) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) least = fminf(least, x[e]);
       }
       float mx = kNegInf;
 #pragma unroll
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[e]);
       mx *= p.scale_log2;
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_run + (kHalf ? kHalfSlack : kSlack)) != 0, 0)) {
-        const float mn = fmaxf(m_run, xgroup_max<2>(mx));
-        const float alpha = mn == kNegInf ? 1.f : exp2_fast(m_run - mn);
+      int then = number + groups;      // the tile whose scores are next
+      const float small = least * p.scale_log2;
+      uint64_t moves = __builtin_amdgcn_ballot_w64(mx > m_run + (kHalf ? kHalfSlack : kSlack));
+      if constexpr (kHalf) moves |= __builtin_amdgcn_ballot_w64(small < m_run + kHalfLeast) | (uint64_t)pending;
+      if (__builtin_expect(moves != 0, 0)) {
+        float mn = xgroup_max<2>(mx), lower = 0.f;
+        if constexpr (kHalf) {
+          // a whole number, so that nothing is rounded where lift is added or taken off and a tile's ranges meet
+          mn = fmaxf(plain ? m_run : m_run + (float)lift, ceilf(mn));
+          if (one(exact || plain ? 1 : 0) == 0 && (lift != 0 || pending != 0 || __builtin_amdgcn_ballot_w64(small < mn + kHalfLeast) != 0)) {
+            // Ranges of weights: from 2^kHalfLeast of the largest on, the 2^kHalfStep below, what is still smaller.  Those that the
+            // tile may have are attended one after the other, m_run as far below the largest score, and the tile's scores computed
+            // again in between.
+            const float a = mn + kHalfLeast, b = a - kHalfStep;
+            const int all = pending != 0 ? pending
+                                         : (__builtin_amdgcn_ballot_w64(mx >= a) != 0 ? 1 : 0) | (__builtin_amdgcn_ballot_w64(small < a && mx >= b) != 0 ? 2 : 0) |
+                                               (__builtin_amdgcn_ballot_w64(small < b) != 0 ? 4 : 0);
+            const int range = all == 0 ? 0 : __builtin_ctz(all);
+            to_come = all & (all - 1);
+            if (to_come != 0) {      // the loop comes to the same tile again
+              then = number--;
+              --k;
+            }
+            lift = kHalfStep * range;
+            const float from = range == 0 ? a : range == 1 ? b : kNegInf, to = range == 0 ? __builtin_nanf("") : range == 1 ? a : b;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {      // a NaN stays
+              const float y = x[e] * p.scale_log2;
+              x[e] = y < from || y >= to ? kNegInf : x[e];
+            }
+          }
+          lower = plain ? 0.f : (float)lift;
+        } else {
+          mn = fmaxf(m_run, mn);
+        }
+        const float alpha = mn - lower == m_run ? 1.f : exp2_fast(m_run - (mn - lower));
         l_run *= alpha;
 #pragma unroll
         for (int a = 0; a < kAccs; ++a) acc[a] *= alpha;
-        m_run = mn;
+        m_run = mn - lower;
       }
       if (kHalf && __builtin_expect(exact, 0)) {
         if (!plain && ((exacts >> (kBuffers + buf)) & 1) != 0) {
           plain = true;
-          l_run *= 1.f / (1 << kPShift);
+          const float to = m_run + (float)lift, f = to == m_run ? 1.f : exp2_fast(m_run - to);
+          m_run = to;
+          l_run *= f / (1 << kPShift);
 #pragma unroll
-          for (int a = 0; a < kAccs; ++a) acc[a] *= 1.f / (1 << (kPShift + Half<FMT>::kVShift));
+          for (int a = 0; a < kAccs; ++a) acc[a] *= f / (1 << (kPShift + Half<FMT>::kVShift));
         }
       }
       const float ms = m_run == kNegInf ? 0.f : kHalf && !plain ? m_run - kPShift : m_run;
@@ -599,7 +659,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
         x = scores(kw);
       } else {
         u32x4_t kw[kSteps];
-        read_k(number + groups, lane, kw);
+        read_k(then, lane, kw);
         // O^T += V^T P^T, V's transpose read as in cache_attend_kernel with 32 rows
         const int li = lane & 15;
         const int vrow = 4 * lq + (li >> 2), chunk = 2 * ((lane >> 4) & 1) + ((li & 3) >> 1);
@@ -646,19 +706,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
             }
         // The reads first; then each product with the vector work that fits beside it: the first half's weights beside the
         // scores, the second's beside the first's products.
-        constexpr int kBeside = kHalf ? 5 : 7;
-        __builtin_amdgcn_sched_group_barrier(0x100, kSteps + 2 * kAccs, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, kHalf ? 17 : 16, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
           __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x2, kBeside, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, kHalf ? 4 : 7, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAccs, 0);
+        
 #pragma unroll
         for (int i = 0; i < kParts * kAccs; ++i) {
           __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x2, kBeside, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, kHalf ? 5 : 7, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x8, kParts * kAccs, 0);
         x = next;
@@ -680,10 +740,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_group_kernel(CacheGr
 
     if (k + 1 == tiles) {      // the piece ends: its states, or its result
       const int lane = hidden(thread & 63), lr = lane & 31, lq = lane >> 5;
-      float m = kHalf && !plain ? m_run - kPShift : m_run, l = xgroup_sum<2>(l_run);
+      float m = m_run, l = xgroup_sum<2>(l_run);
+      if constexpr (kHalf) {      // without the factors, which are powers of two
+        const int up = plain ? 0 : kPShift + lift;
+        const float f = __uint_as_float((uint32_t)(127 - up) << 23);
+        m += plain ? 0.f : (float)lift;
+        l *= f;
 #pragma unroll
-      for (int a = 0; a < kAccs; ++a)
-        if constexpr (kHalf) acc[a] *= plain ? 1.f : 1.f / (1 << Half<FMT>::kVShift);
+        for (int a = 0; a < kAccs; ++a) acc[a] *= plain ? 1.f : f / (1 << Half<FMT>::kVShift);
+      }
       auto piece_of = [&](int c) {
         return f32x4_t{acc[c >> 2][4 * (c & 3)], acc[c >> 2][4 * (c & 3) + 1], acc[c >> 2][4 * (c & 3) + 2], acc[c >> 2][4 * (c & 3) + 3]};
       };
