@@ -475,7 +475,7 @@ ss_status ss_cache_attend_window(const ss_cache_desc *desc, const void *pages, c
 /* How rows are turned by their positions: of each head the first rotary_dim
  * channels, in pairs (j, j + rotary_dim / 2) or, interleaved, (2j, 2j + 1), pair j by
  * the angle position * inv_freq[j]; y1 = scale (x1 cos - x2 sin), y2 = scale (x2 cos +
- * x1 sin).  The other channels stay as they are, bit for bit.  Angles are below 2^50. */
+ * x1 sin).  The other channels stay as they are, bit for bit.  Angles are below 2^48. */
 typedef struct {
   int32_t rotary_dim;       /* a multiple of 16, 16..128 (others up to 128: SS_ERR_UNSUPPORTED) */
   int32_t interleaved;      /* 0 or 1                                          */

@@ -5,6 +5,7 @@
 
 #include "ss_cache.h"
 #include "ss_cache_device.h"
+#include "ss_turn.h"
 
 namespace ss {
 namespace {
@@ -29,26 +30,6 @@ namespace {
 // written, 389 us, 4.3 TB/s; a large copy 4.9); drafted rows the angles' 30 products of 64 bits each and a launch (16 requests of 16
 // to 48 rows, 64 + 8 heads in bf16 8.4 us; every lane its own eight angles 10.3).
 // ---------------------------------------------------------------------------
-
-// cos and sin of p f.
-__device__ __forceinline__ void turn_of(double p, float f, double scale, double &c, double &s) {
-  const double a = p * (double)f, n = __builtin_rint(a * 0.63661977236758134);                            // 2 / pi
-  const double x = __builtin_fma(-n, 6.123233995736766e-17, __builtin_fma(-n, 1.5707963267948966, a));      // pi / 2 in two parts
-  const double y = x * x;
-  const int q = (int)(n - 4.0 * __builtin_floor(n * 0.25));
-  double u = __builtin_fma(y, -1.0 / 39916800, 1.0 / 362880), v = __builtin_fma(y, 1.0 / 479001600, -1.0 / 3628800);
-  u = __builtin_fma(y, u, -1.0 / 5040);
-  u = __builtin_fma(y, u, 1.0 / 120);
-  u = __builtin_fma(y, u, -1.0 / 6);
-  v = __builtin_fma(y, v, 1.0 / 40320);
-  v = __builtin_fma(y, v, -1.0 / 720);
-  v = __builtin_fma(y, v, 1.0 / 24);
-  v = __builtin_fma(y, v, -0.5);
-  const double sx = __builtin_fma(x * y, u, x), cx = __builtin_fma(y, v, 1.0);
-  const double k = q & 1 ? sx : cx, l = q & 1 ? cx : sx;
-  c = scale * ((q + 1) & 2 ? -k : k);
-  s = scale * (q & 2 ? -l : l);
-}
 
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
