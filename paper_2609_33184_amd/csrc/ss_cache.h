@@ -63,9 +63,9 @@ struct CacheAttendArgs : CacheArgs {
   int64_t q_row_stride;
   float *out, *lse;                     // lse may be null
   const float *prev_out, *prev_lse;     // both or neither
-  float *part_a, *part_ml;              // states of the pieces: [2 workers][M][128], [2 workers][M][2]
+  float *part_a, *part_ml;              // states of the pieces: [2 workers][rows][128], [2 workers][rows][2]; rows: M, of a block in groups
   int32_t Hq, G;
-  uint32_t g_inv;                       // ceil(65536 / G): r / G = r * g_inv >> 16 for r < 64, G <= 64
+  uint32_t g_inv;                       // ceil(65536 / G): r / G = r * g_inv >> 16 where r * G < 65536 (r < 512, G <= 64)
   int32_t M;                            // rows per KV head: max_rows * G
   int32_t workers;                      // shares that the call's units are cut into
   int32_t alone;                        // a worker is a wave, not a workgroup
@@ -97,25 +97,29 @@ struct CacheSplit {
 };
 CacheSplit cache_attend_split(int fmt, int B, int Hkv, int capacity, int M);
 // From how many rows per KV head on the rows of a tree are attended in groups, and how that is split.
-// 16 x 32768 tokens with 40 and 64 rows in bf16 450 and 468 us, with waves for themselves 495 and 513; in 8
-// bits 523 and 525, 354 and 371; 96 rows 530 and 707.
+// 16 x 32768 tokens with 40 and 64 rows in bf16 465 and 481 us, with waves for themselves 516 and 528; in 8
+// bits 587 and 595, 368 and 385; in 4 bits 566 and 568, 311 and 324; 96 rows in 8 bits 617 and, as two blocks of waves, 707.
 constexpr int cache_group_rows(int fmt) { return fmt == kCacheBf16 ? 33 : 65; }
 CacheSplit cache_group_split(int fmt, int B, int Hkv, int capacity, int M);
 // Into how many parts of as many tiles (of 32 tokens) each of `wholes` (request, KV head, block of rows) is cut, a workgroup to a
 // part, with at most `most` workgroups; 1: nothing to join; 0: cut by the lengths, into equal shares of all the units.
-// Few tiles are not cut.  One request, 8 KV heads, 64 rows on 32 heads in bf16: 4 tiles 14.8 us, cut 16.9; 8 tiles 20.1 and 18.9;
-// 16 tiles 31.6 and 21.5.  16 requests of one row over 10 tiles 11.5 and 15.5; 8 of 64 rows over 8 tiles 23.6 and 34.3.
-// Where a window makes the lengths alike, equal parts are as even as equal shares and none straddles two requests: 16 requests of 8
-// rows, 64 per KV head, in a window of 1024 29.3 us, shares 34.4; 64 requests of one row in a window of 4096 in bf16 162 and 171;
-// trees of 32 rows, 128 per KV head, in one of 4096 94.9 and 101.4.
-// Not where a part would be long: a single full window among short requests takes as long as its part, 50 us for 129 tiles.
-inline int cache_attend_parts(int64_t tiles, int64_t wholes, int64_t most, bool alike) {
+// Few tiles are not cut.  One request, 8 KV heads, 64 rows on 32 heads in bf16: 4 tiles 14.1 us, cut 16.5; 8 tiles 19.2 and 17.9;
+// 16 tiles 29.4 and 18.6.  16 requests of one row over 10 tiles 11.4 and 15.8.
+// Where a window makes the lengths alike, equal parts save the 2 to 5 us in which a worker finds its share.  The lengths themselves lie on
+// the device, though, and where one request fills its window and the others hold 40 tokens the call waits for its parts' workgroups
+// alone.  So parts are short.  Parts and shares, us, all windows full and one alone:
+//   16 requests of 8 rows, 64 per KV head, 4 bits, window 1024 (18 tiles a part) 28.5, 32.9 and 26.2, 23.3; 4096 (66) 61.8, 58.0 and 59.7, 30.3
+//   64 requests of one row, bf16, window 512 (18) 27.7, 30.1 and 18.5, 19.4; 1024 (34) 45.7, 48.0 and 29.4, 19.1; 4096 (132) 168, 171 and 90.6, 26.1
+//   16 trees of 32 rows, 128 per KV head, 8 bits, window 1024 (9) 43.8, 45.7 and 39.4, 31.3; 2048 (17) 62.0, 65.2 and 55.6, 35.7; 4096 (33) 95.8,
+//   98.6 and 89.6, 42.8
+constexpr int kCachePartTiles = 20, kCacheGroupPartTiles = 10;     // of the longest part
+inline int cache_attend_parts(int64_t tiles, int64_t wholes, int64_t most, bool alike, bool group) {
   if (tiles <= (wholes < 64 ? 4 : 16)) return 1;
   if (!alike) return 0;
   int64_t parts = most / wholes;
   parts = parts > tiles / 4 ? tiles / 4 : parts;
   parts = parts < 1 ? 1 : parts;
-  return (tiles + parts - 1) / parts <= 160 ? (int)parts : 0;
+  return (tiles + parts - 1) / parts <= (group ? kCacheGroupPartTiles : kCachePartTiles) ? (int)parts : 0;
 }
 
 // Launch wrappers; return hipGetLastError() of the launch.

@@ -12,11 +12,11 @@ namespace {
 
 // the attention counts the requests in chunks of 64, one lane for each of 64 chunks at most
 static_assert(SS_CACHE_MAX_REQUESTS <= ss::kCacheMaxRequests && ss::kCacheMaxRequests <= 64 * 64, "requests beyond a wave's chunks would be dropped");
-// a workgroup of 256 threads takes 16 rows
 // a row's word has a bit for every node; keeping a path holds a tree's rows in registers
 static_assert(SS_CACHE_MAX_TREE == ss::kCacheMaxTree && SS_CACHE_MAX_TREE == 64, "nodes of a tree are bits of 64");
 // rows of a KV head are divided by G with a multiplication, exact where row x G < 2^16
 static_assert(SS_CACHE_MAX_TREE_ROWS_PER_KV_HEAD * SS_MAX_ROWS_PER_KV_HEAD < 65536, "a row's query and head come from a multiplication");
+// a workgroup of 256 threads takes 16 rows
 static_assert(((int64_t)SS_CACHE_MAX_ROWS + 15) / 16 * 256 < (int64_t(1) << 32), "a launch's threads are counted in 32 bits");
 
 using ss::fail;
@@ -172,10 +172,10 @@ void fill_seen(ss::CacheSeenArgs *p, const ss_cache_desc *d, const AttendLayout 
   // a window's tokens begin and end within a tile, and so do the first ones
   if (window > 0 && (int64_t)window + sinks + d->max_rows < reach) reach = (int64_t)window + sinks + d->max_rows + 3 * ss::kCacheTile;
   const int wholes = p->B * p->Hkv * layout.blocks;
-  // two workgroups a CU for groups (16 trees of 32 rows in a window of 4096 93 us, one 131), else one (32 requests of one row in a
-  // window of 1024 29.5, two 31.0)
+  // workgroups a CU: two for groups (16 trees of 32 rows in a window of 1024 43.3 us, with one, whose parts are too long, 45.7), else one
+  // (16 requests of 8 rows, 64 per KV head, in a window of 1024 28.0, two 29.3)
   const int fill = layout.group ? 512 : 256, most = p->workers < fill ? p->workers : fill;
-  p->parts = layout.split.alone ? 0 : ss::cache_attend_parts((reach + ss::kCacheTile - 1) / ss::kCacheTile, wholes, most, reach < p->capacity);
+  p->parts = layout.split.alone ? 0 : ss::cache_attend_parts((reach + ss::kCacheTile - 1) / ss::kCacheTile, wholes, most, reach < p->capacity, layout.group);
   if (p->parts > 0) p->workers = wholes * p->parts;
 }
 
