@@ -27,8 +27,8 @@ namespace {
 // for bit the one that the rotated rows' ss_cache_write gives.
 //
 // What bounds it: filling prompts, memory (16 of 2048 to 8191 rows, 32 + 8 heads, 8 bits: 1.7 GB read and
-// written, 389 us, 4.3 TB/s; a large copy 4.9); drafted rows the angles' 30 products of 64 bits each and a launch (16 requests of 16
-// to 48 rows, 64 + 8 heads in bf16 8.4 us; every lane its own eight angles 10.3).
+// written, 389 us, 4.3 TB/s; a large copy 4.9); drafted rows a launch and the angles' 30 products of 64 bits each, which the 40 workgroups
+// of 16 rows repeat (16 requests of 16 to 48 rows, 64 + 8 heads in bf16 8.4 us; every lane its own eight angles 10.3).
 // ---------------------------------------------------------------------------
 
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
@@ -141,7 +141,10 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheAppendArgs 
   }
 }
 
-constexpr int64_t kFewRows = 1 << 14;      // rows x KV heads up to which a workgroup takes one head, as for a write
+// Rows x KV heads up to which a workgroup takes one KV head or two query heads, beyond four and eight, since all of a row's
+// workgroups compute the same sines: with 8 KV heads one and four, in the kernel, 64 rows 4.2 and 5.2 us, 256 rows 5.3 and 6.1, 480 rows
+// with 64 query heads 8.1 and 8.5; 1024 rows 9.4 and 8.8, 2048 rows 16.6 and 11.8.
+constexpr int64_t kFewRows = 1 << 12;
 
 template <int FMT>
 hipError_t append(const CacheAppendArgs &p, hipStream_t s) {
