@@ -338,7 +338,12 @@ class PagedCache:
 
     ``tree_rows``: most nodes of a request's tree of drafted tokens (0: none).
     A step with trees is ``grow``, ``append`` (or ``write``), ``attend_tree``
-    and ``keep``."""
+    and ``keep``.
+
+    ``row_start``: where each request's rows begin, and the last one's end.
+    Without it every request has ``max_rows`` rows, in ``attend_tree``
+    ``tree_rows``: a step whose calls take one batch of trees gives it, unless
+    the two are one number."""
 
     def __init__(self, num_requests: int, num_q_heads: int, num_kv_heads: int, max_tokens: int, fmt: int = ss.SS_CACHE_MXFP8,
                  page_tokens: int = 64, num_pages: Optional[int] = None, max_rows: int = 1,
