@@ -180,10 +180,10 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs p) {
 // sinks' and, behind the gap, the windows' (Sight); a tile that all rows see whole
 // needs no mask, of the others a word of 32 bits says which tokens a row sees.
 // Where a window makes the lengths alike the call is cut into equal parts of each
-// request instead of equal shares (cache_attend_parts).  64 requests of one row in a
-// window of 4096 in bf16 (1.03 GB) 162 us, 6.3 TB/s; 16 requests of 8 rows, 64 per KV
-// head, in a window of 1024 in 4 bits 26.0 us and 5.1 for the join, of which the
-// SIMDs issue half and the rest is the latency of the first loads and of the merge.
+// request instead of equal shares while they are short (cache_attend_parts).  64 requests
+// of one row in a window of 4096 in bf16 (1.03 GB) 170 us, 6.0 TB/s; 16 requests of 8
+// rows, 64 per KV head, in a window of 1024 in 4 bits 27.0 us, in a trace 25.5 and 5.0 for
+// the join: nine steps of two tiles, of which the SIMDs issue a third and the rest is latency.
 // ---------------------------------------------------------------------------
 constexpr int kLdsRow = 256;                        // a staged V row, bf16
 constexpr int kVTile = kCacheTile * kLdsRow;

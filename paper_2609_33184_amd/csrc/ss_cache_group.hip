@@ -24,11 +24,12 @@
 // bf16 rows go from memory to LDS without passing registers.  What a wave needs next is waited for by
 // count, so that the loads behind it stay in flight.
 //
-// What bounds it.  bf16, 16 x 12000..16384 tokens, 256 rows: 520 us; the SIMDs issue vector work 45% and
-// matrix work 47% of the cycles, one after the other, at 1.65 GHz; the matrix work alone would take 185 us of the formula and
-// twice that in three parts.  8 bits, 16 x 32768 tokens, 96 rows: 530 us, 155 for the bytes; vector work 37%,
-// matrix work 31% on three SIMDs of four (96 rows leave a wave without), the rest waits at the barrier and for LDS.  One
-// request of 32768 tokens, 256 rows: 92 us and 10.5 for the join of its 32 states a row.
+// What bounds it (whole calls, the join in them; shares of the cycles from a trace of the kernel alone).  bf16, 16 x 12000..16384
+// tokens, 256 rows: 503 to 522 us; the SIMDs issue vector work 48% and matrix work 47% of the cycles, one after the other; the
+// matrix work alone would take 382.  8 bits, 16 x 32768 tokens, 96 rows: 617 us, 155 for the bytes, 344 for the matrix work, all of it on
+// three SIMDs of four (96 rows leave a wave without): vector work 35%, matrix work 27% of all four's cycles, and the rest waits at the
+// barrier and for LDS.  One request of 32768 tokens, 256 rows: 99 us, 57 for the matrix work, 10 for the join of its 32 states a
+// row.  None of it depends on the scores or the values.
 #include <hip/hip_runtime.h>
 
 #include "ss_cache.h"
@@ -46,7 +47,7 @@ constexpr int kBuffers = 4;                     // tiles in LDS
 constexpr int kSteps = kCacheDim / 16;          // of a product over the channels
 constexpr int kAccs = kCacheDim / 32;           // accumulators of 32 channels
 
-// What a piece costs beside its tiles, in tiles: 24 ragged requests with 4, 8 and 16 52.7, 53.4 and 63.6 us.
+// What a piece costs beside its tiles, in tiles: 24 ragged requests with 4, 8 and 16 54.0, 55.9 and 62.8 us.
 constexpr int kPieceGroupTiles = 8;
 
 template <int I>
